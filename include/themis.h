@@ -482,6 +482,143 @@ enum {
 };
 int themis_classify_batch(const themis_batch_t *batch, uint8_t *classes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Gradients of an iteration
+ *
+ * The collectives that the entry points above evaluate carry the gradients of
+ * a training iteration.  The ones below work on these gradients, on the rank:
+ * rows of a token table and the table's gradient (in a language model the
+ * largest tensor of the iteration, and the last to become ready), the norm of
+ * all gradients, and their clipped copies in the flat buckets whose bytes are
+ * size_bytes / coll_size of a batch.  The conventions are the same: device
+ * pointers, caller-owned memory, kernels enqueued on `stream` and no
+ * synchronisation, a status for what the host can see.  Results are the same
+ * in every call on the same inputs: no sum's order is left to chance.
+ * ------------------------------------------------------------------------- */
+
+/* Element types: IEEE binary32, bfloat16, IEEE binary16; token numbers. */
+enum { THEMIS_F32 = 0, THEMIS_BF16 = 1, THEMIS_F16 = 2, THEMIS_I32 = 3, THEMIS_I64 = 4 };
+
+/*
+ * Rows in device memory, in two levels (sequences of tokens, say): row r
+ * begins (r / inner) * outer_stride + (r % inner) * inner_stride elements
+ * behind data.  The elements of a row are adjacent.  Token numbers are rows of
+ * one element.  Strides may be 0 or negative in what is only read.  data needs
+ * the alignment of its element type and no more.
+ */
+typedef struct themis_rows {
+  void *data;
+  int32_t type;         /* THEMIS_F32 .. THEMIS_I64                           */
+  uint64_t inner;       /* rows of the inner level, >= 1                      */
+  int64_t outer_stride; /* elements                                           */
+  int64_t inner_stride;
+} themis_rows_t;
+
+/*
+ * themis_embedding_lookup -- rows of a table by number, scaled:
+ *   out[t][j] = scale * table[ids[t]][j]        t < n, j < width
+ * The product is made in binary32 and rounded once to out's type.  A number
+ * outside 0 .. vocab-1 gives a row of NaN (the call does not fail).
+ *
+ *   table : vocab rows of `width` elements, THEMIS_F32 / _BF16 / _F16
+ *   ids   : n token numbers, THEMIS_I32 / _I64
+ *   out   : n rows of `width`, any of the three types; rows must not overlap
+ *           each other nor the inputs.
+ * vocab, n and width below 2^31, else THEMIS_ERR_UNSUPPORTED.
+ */
+int themis_embedding_lookup(const themis_rows_t *table, uint64_t vocab, uint64_t width,
+                            const themis_rows_t *ids, uint64_t n, float scale,
+                            const themis_rows_t *out, void *stream);
+
+/*
+ * themis_embedding_grad -- the gradient of the table behind it:
+ *   grad[v][j] = (accumulate ? grad[v][j] : 0) +
+ *                scale * sum of grad_out[t][j] over the t with ids[t] == v
+ * Sums are made in binary32 in an order that the token numbers alone decide,
+ * and rounded once to grad's type.  Tokens of number `ignored` (padding; -1 for
+ * none) and those outside 0 .. vocab-1 have no gradient: their rows of grad_out
+ * are not read.  Without `accumulate` every row of grad is written, those of
+ * numbers that do not occur with zeros; with it, only rows of numbers that
+ * occur are read or written.
+ *
+ *   grad_out  : n rows of `width`, THEMIS_F32 / _BF16 / _F16
+ *   ids       : n token numbers, THEMIS_I32 / _I64
+ *   grad      : vocab rows of `width`, any of the three types; rows must not
+ *               overlap each other nor the inputs.
+ *   workspace : themis_embedding_grad_workspace_bytes(n, width, vocab) bytes,
+ *               16-byte aligned, untouched until the stream has drained, one
+ *               per call in flight.
+ * vocab, n and width below 2^31, else THEMIS_ERR_UNSUPPORTED.
+ */
+size_t themis_embedding_grad_workspace_bytes(uint64_t n, uint64_t width, uint64_t vocab);
+int themis_embedding_grad(const themis_rows_t *grad_out, uint64_t width,
+                          const themis_rows_t *ids, uint64_t n, float scale, int64_t ignored,
+                          int accumulate, const themis_rows_t *grad, uint64_t vocab,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One view of a gradient: element (r, c) is in[r * in_row_stride +
+ * c * in_col_stride].  A tensor may be given as several parts (one after the
+ * other, the same `tensor`): more dimensions than two, say.  out may be in
+ * itself (same type and strides), NULL where only norms are wanted, or memory
+ * of any of the three types that overlaps no other part.
+ */
+typedef struct themis_gradient {
+  const void *in;
+  void *out;
+  uint32_t tensor; /* 0 .. n_tensors-1, not smaller than the part before's */
+  int32_t in_type;  /* THEMIS_F32, _BF16, _F16 */
+  int32_t out_type;
+  uint64_t rows, cols;
+  int64_t in_row_stride, in_col_stride;   /* elements */
+  int64_t out_row_stride, out_col_stride;
+} themis_gradient_t;
+
+/*
+ * themis_gradient_plan -- lays out a list of gradients for the kernels: host
+ * work, made once for as long as the tensors stay where they are.
+ *
+ *   plan  : filled in; `image` is left NULL.
+ *   image : NULL (only sizes are wanted) or image_bytes of HOST memory.
+ * The caller copies the image to device memory (16-byte aligned) and puts its
+ * address into plan->image.
+ */
+typedef struct themis_gradient_plan {
+  uint64_t n_tensors;
+  uint64_t n_pieces;
+  uint64_t image_bytes;
+  uint64_t workspace_bytes; /* of themis_gradient_norm / _clip              */
+  uint32_t has_out;         /* every part has an out                        */
+  uint32_t strided;         /* some part is not one run of adjacent elements */
+  const void *image;        /* device copy of the image                     */
+} themis_gradient_plan_t;
+int themis_gradient_plan(const themis_gradient_t *parts, uint64_t n_parts, uint64_t n_tensors,
+                         themis_gradient_plan_t *plan, void *image, size_t image_bytes);
+
+/*
+ * themis_gradient_norm -- Euclidean norms:
+ *   norms[i] = sqrt(sum of squares of tensor i)     (NULL: not wanted)
+ *   total[0] = sqrt(sum of squares of all tensors)
+ * Squares and sums are binary64, so that no binary32 value's square overflows
+ * or vanishes; the results are binary32.  NaN or infinite elements give NaN or
+ * infinite norms.  A tensor without elements, and an empty list, have norm 0.
+ *
+ * themis_gradient_clip -- the same, and
+ *   out = in * factor,   factor = max_norm / total if total > max_norm, else 1
+ *   total[1] = factor
+ * The product is made in binary32 and rounded once to out's type.  With a NaN
+ * norm the factor is NaN, with an infinite one 0.  max_norm is positive and
+ * finite.  Gradients that are their own out are left alone where the factor
+ * is 1.
+ *
+ *   workspace : plan->workspace_bytes, 16-byte aligned, untouched until the
+ *               stream has drained, one per call in flight.
+ */
+int themis_gradient_norm(const themis_gradient_plan_t *plan, float *total, float *norms,
+                         void *workspace, size_t workspace_bytes, void *stream);
+int themis_gradient_clip(const themis_gradient_plan_t *plan, double max_norm, float *total,
+                         float *norms, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

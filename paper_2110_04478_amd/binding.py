@@ -33,6 +33,24 @@ class _Batch(C.Structure):
     ]
 
 
+class _Rows(C.Structure):
+    _fields_ = [("data", _vp), ("type", C.c_int32), ("inner", C.c_uint64),
+                ("outer_stride", C.c_int64), ("inner_stride", C.c_int64)]
+
+
+class _Gradient(C.Structure):
+    _fields_ = [("in_", _vp), ("out", _vp), ("tensor", C.c_uint32), ("in_type", C.c_int32),
+                ("out_type", C.c_int32), ("rows", C.c_uint64), ("cols", C.c_uint64),
+                ("in_row_stride", C.c_int64), ("in_col_stride", C.c_int64),
+                ("out_row_stride", C.c_int64), ("out_col_stride", C.c_int64)]
+
+
+class _GradientPlan(C.Structure):
+    _fields_ = [("n_tensors", C.c_uint64), ("n_pieces", C.c_uint64), ("image_bytes", C.c_uint64),
+                ("workspace_bytes", C.c_uint64), ("has_out", C.c_uint32), ("strided", C.c_uint32),
+                ("image", _vp)]
+
+
 _lib = None
 
 
@@ -87,6 +105,23 @@ def lib():
         L.themis_sweep_with_scratch.restype = C.c_int
         L.themis_sweep_with_scratch.argtypes = [C.POINTER(_Batch), C.c_int, _vp, C.c_int, C.c_uint,
                                                 _vp, _vp, C.c_size_t, _vp, C.c_size_t, _vp]
+        L.themis_embedding_lookup.restype = C.c_int
+        L.themis_embedding_lookup.argtypes = [C.POINTER(_Rows), C.c_uint64, C.c_uint64, C.POINTER(_Rows),
+                                              C.c_uint64, C.c_float, C.POINTER(_Rows), _vp]
+        L.themis_embedding_grad_workspace_bytes.restype = C.c_size_t
+        L.themis_embedding_grad_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.c_uint64]
+        L.themis_embedding_grad.restype = C.c_int
+        L.themis_embedding_grad.argtypes = [C.POINTER(_Rows), C.c_uint64, C.POINTER(_Rows), C.c_uint64,
+                                            C.c_float, C.c_int64, C.c_int, C.POINTER(_Rows), C.c_uint64,
+                                            _vp, C.c_size_t, _vp]
+        L.themis_gradient_plan.restype = C.c_int
+        L.themis_gradient_plan.argtypes = [C.POINTER(_Gradient), C.c_uint64, C.c_uint64,
+                                           C.POINTER(_GradientPlan), _vp, C.c_size_t]
+        L.themis_gradient_norm.restype = C.c_int
+        L.themis_gradient_norm.argtypes = [C.POINTER(_GradientPlan), _vp, _vp, _vp, C.c_size_t, _vp]
+        L.themis_gradient_clip.restype = C.c_int
+        L.themis_gradient_clip.argtypes = [C.POINTER(_GradientPlan), C.c_double, _vp, _vp, _vp,
+                                           C.c_size_t, _vp]
         _lib = L
     return _lib
 
@@ -357,3 +392,206 @@ def alloc_workspace(nbytes: int, device="cuda:0") -> Optional[torch.Tensor]:
     if nbytes <= 0:
         return None
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+# -- gradients of an iteration ------------------------------------------------------------
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int32: 3, torch.int64: 4}
+INVALID_ARGUMENT = -1
+
+
+def _rows(t: torch.Tensor, lead: int) -> Optional[_Rows]:
+    """t as rows of its last dimension (lead = t.dim() - 1) or of single elements (lead =
+    t.dim()), in the two levels of themis_rows; None where its strides need more."""
+    if lead < t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
+        return None
+    if t.is_contiguous():
+        step = t.shape[-1] if lead < t.dim() else 1
+        return _Rows(t.data_ptr(), _TYPES[t.dtype], max(1, t.numel()), 0, step)
+    levels = []   # (rows, stride), outermost first, merged where one stride covers both
+    for n, s in zip(t.shape[:lead], t.stride()[:lead]):
+        if n == 1:
+            continue
+        if levels and levels[-1][1] == n * s:
+            levels[-1] = (levels[-1][0] * n, s)
+        else:
+            levels.append((n, s))
+    if len(levels) > 2:
+        return None
+    outer = levels[0][1] if len(levels) == 2 else 0
+    inner, step = levels[-1] if levels else (1, 0)
+    return _Rows(t.data_ptr(), _TYPES[t.dtype], max(1, inner), outer, step)
+
+
+def _need(ok: bool):
+    if not ok:
+        raise ThemisError(INVALID_ARGUMENT)
+
+
+def _is_float(t: torch.Tensor) -> bool:
+    return _TYPES.get(t.dtype, 9) < 3
+
+
+def _is_index(t: torch.Tensor) -> bool:
+    return t.dtype in (torch.int32, torch.int64)
+
+
+def _read_rows(t: torch.Tensor, lead: int) -> tuple:
+    """(rows, the tensor that holds them): t itself, or a copy where its strides are beyond
+    what the library reads."""
+    r = _rows(t, lead)
+    if r is None:
+        t = t.contiguous()
+        r = _rows(t, lead)
+    return r, t
+
+
+def themis_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
+                            out: Optional[torch.Tensor] = None,
+                            out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """scale * table[ids] -> [*ids.shape, width] of out's type (given by out or out_dtype;
+    the table's otherwise).  A token number outside the table gives a row of NaN."""
+    _need(table.dim() == 2 and _is_float(table) and _is_index(ids) and
+          table.device == ids.device and table.is_cuda)
+    vocab, width = table.shape
+    if out is None:
+        out = torch.empty((*ids.shape, width), dtype=out_dtype or table.dtype, device=table.device)
+    _need(_is_float(out) and out.shape == (*ids.shape, width) and out.device == table.device and
+          out_dtype in (None, out.dtype))
+    n = ids.numel()
+    if n == 0 or width == 0:
+        return out
+    rows_t, table = _read_rows(table, 1)
+    rows_i, ids = _read_rows(ids, ids.dim())
+    rows_o = _rows(out, out.dim() - 1)
+    _need(rows_o is not None)
+    _check(lib().themis_embedding_lookup(rows_t, vocab, width, rows_i, n, scale, rows_o, _stream()))
+    return out
+
+
+def themis_embedding_grad_workspace_bytes(n: int, width: int, vocab: int) -> int:
+    return lib().themis_embedding_grad_workspace_bytes(n, width, vocab)
+
+
+def themis_embedding_grad(grad_out: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0,
+                          ignored: int = -1, out: Optional[torch.Tensor] = None,
+                          out_dtype: Optional[torch.dtype] = None, accumulate: bool = False,
+                          workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of the table behind themis_embedding_lookup -> [vocab, width] of out's type
+    (given by out or out_dtype; grad_out's otherwise), or added to out where `accumulate`.
+    Tokens of number `ignored`, or outside the table, have no gradient."""
+    _need(_is_float(grad_out) and _is_index(ids) and grad_out.shape[:-1] == ids.shape and
+          grad_out.dim() >= 1 and grad_out.device == ids.device and grad_out.is_cuda and
+          vocab >= 0 and (out is not None or not accumulate))
+    width = grad_out.shape[-1]
+    if out is None:
+        out = torch.empty((vocab, width), dtype=out_dtype or grad_out.dtype, device=grad_out.device)
+    _need(_is_float(out) and out.shape == (vocab, width) and out.device == grad_out.device and
+          out_dtype in (None, out.dtype))
+    n = ids.numel()
+    if vocab == 0 or width == 0 or (n == 0 and accumulate):
+        return out
+    rows_g, grad_out = _read_rows(grad_out, grad_out.dim() - 1)
+    rows_i, ids = _read_rows(ids, ids.dim())
+    rows_o = _rows(out, 1)
+    _need(rows_o is not None)
+    if workspace is None:
+        workspace = alloc_workspace(themis_embedding_grad_workspace_bytes(n, width, vocab), out.device)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().themis_embedding_grad(rows_g, width, rows_i, n, scale, ignored, int(accumulate),
+                                       rows_o, vocab, _ptr(workspace), ws_bytes, _stream()))
+    return out
+
+
+@dataclass
+class GradientPlan:
+    """A list of gradients laid out for themis_gradient_norm / _clip.  It keeps the tensors, the
+    device copy of the layout and the workspace, so calls on one plan must follow each other (one
+    stream, or the caller's own ordering)."""
+    grads: list
+    out: Optional[list]
+    image: torch.Tensor
+    workspace: Optional[torch.Tensor]
+    c_struct: _GradientPlan
+    n_tensors: int
+
+    @property
+    def device(self):
+        return self.image.device
+
+
+def _views(g: torch.Tensor, o: Optional[torch.Tensor]):
+    """g (and o, element for element) as views of two levels: yields (in offset, out offset,
+    rows, cols, in row stride, in col stride, out row stride, out col stride), in elements."""
+    so = o.stride() if o is not None else g.stride()
+    dims = sorted(((abs(a), abs(b), n, a, b) for n, a, b in zip(g.shape, g.stride(), so) if n != 1),
+                  reverse=True)
+    merged = []   # (count, in stride, out stride), the longest steps first
+    for _, _, n, a, b in dims:
+        if merged and merged[-1][1] == n * a and merged[-1][2] == n * b:
+            merged[-1] = (merged[-1][0] * n, a, b)
+        else:
+            merged.append((n, a, b))
+    while len(merged) < 2:
+        merged.insert(0, (1, 0, 0))
+    offsets = [(0, 0)]
+    for n, a, b in merged[:-2]:
+        offsets = [(x + k * a, y + k * b) for x, y in offsets for k in range(n)]
+    (rows, ra, rb), (cols, ca, cb) = merged[-2:]
+    for x, y in offsets:
+        yield x, y, rows, cols, ra, ca, rb, cb
+
+
+def themis_gradient_plan(grads, out=None) -> GradientPlan:
+    """Lays out a list of gradients for themis_gradient_norm and themis_gradient_clip.
+
+    out: where the clipped gradients go, tensors of the gradients' shapes and any of the three
+    types (parts of a flat bucket, say); the gradients themselves where it is not given.  Good
+    for as long as the tensors stay where they are; their values may change."""
+    grads = list(grads)
+    _need(all(_is_float(g) and g.is_cuda for g in grads) and
+          len({g.device for g in grads}) <= 1)
+    outs = grads if out is None else list(out)
+    _need(len(outs) == len(grads) and
+          all(_is_float(o) and o.shape == g.shape and o.device == g.device for g, o in zip(grads, outs)))
+    # (a gradient that is its own target and has elements in one place cannot be scaled there:
+    # then only its norm is to be had)
+    no_out = out is None and any(s == 0 and n > 1 for g in grads for n, s in zip(g.shape, g.stride()))
+    parts = []
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        if g.numel() == 0:
+            continue
+        gt, ot, ge, oe = _TYPES[g.dtype], _TYPES[o.dtype], g.element_size(), o.element_size()
+        for x, y, rows, cols, ra, ca, rb, cb in _views(g, o):
+            parts.append(_Gradient(g.data_ptr() + x * ge, None if no_out else o.data_ptr() + y * oe, i,
+                                   gt, ot, rows, cols, ra, ca, rb, cb))
+    array = (_Gradient * len(parts))(*parts)
+    plan = _GradientPlan()
+    _check(lib().themis_gradient_plan(array, len(parts), len(grads), plan, None, 0))
+    image = np.empty((plan.image_bytes + 7) // 8, dtype=np.uint64)
+    _check(lib().themis_gradient_plan(array, len(parts), len(grads), plan, image.ctypes.data,
+                                      image.nbytes))
+    device = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
+    on_device = torch.from_numpy(image.view(np.int64)).to(device)
+    plan.image = on_device.data_ptr()
+    return GradientPlan(grads, None if out is None else outs, on_device,
+                        alloc_workspace(plan.workspace_bytes, device), plan, len(grads))
+
+
+def themis_gradient_norm(plan: GradientPlan):
+    """Euclidean norms -> (total f32[1], norms f32[n_tensors])."""
+    result = torch.empty(1 + plan.n_tensors, dtype=torch.float32, device=plan.device)
+    total, norms = result[:1], result[1:]
+    _check(lib().themis_gradient_norm(plan.c_struct, total.data_ptr(), norms.data_ptr(),
+                                      _ptr(plan.workspace), plan.c_struct.workspace_bytes, _stream()))
+    return total, norms
+
+
+def themis_gradient_clip(plan: GradientPlan, max_norm: float):
+    """The same, and the gradients times min(1, max_norm / norm) into the plan's targets
+    -> (f32[2]: norm and factor, norms f32[n_tensors])."""
+    result = torch.empty(2 + plan.n_tensors, dtype=torch.float32, device=plan.device)
+    total, norms = result[:2], result[2:]
+    _check(lib().themis_gradient_clip(plan.c_struct, float(max_norm), total.data_ptr(), norms.data_ptr(),
+                                      _ptr(plan.workspace), plan.c_struct.workspace_bytes, _stream()))
+    return total, norms

@@ -4,12 +4,13 @@ import glob
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 PKG = os.path.dirname(HERE)
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libthemis_hip.so")
-SOURCES = [os.path.join(HERE, "themis_api.hip")]
+SOURCES = [os.path.join(HERE, "themis_api.hip"), os.path.join(HERE, "themis_gradients_api.hip")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -38,8 +39,14 @@ def stale() -> bool:
 def build(force: bool = True, extra=()) -> str:
     if not force and not stale():
         return LIB
-    cmd = [HIPCC, *FLAGS, *extra, "-o", LIB, *SOURCES]
-    subprocess.run(cmd, check=True)
+    # one compiler for each source, side by side: the event loops take minutes
+    with tempfile.TemporaryDirectory(dir=HERE) as work:
+        objects = [os.path.join(work, os.path.basename(s) + ".o") for s in SOURCES]
+        compilers = [subprocess.Popen([HIPCC, *[f for f in FLAGS if f != "-shared"], *extra, "-c", "-o", o, s])
+                     for s, o in zip(SOURCES, objects)]
+        if any([c.wait() for c in compilers]):
+            raise RuntimeError("hipcc failed")
+        subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-o", LIB, *objects], check=True)
     return LIB
 
 
@@ -81,8 +88,9 @@ def exec_hazards(asm_text: str):
 def device_assembly() -> str:
     """The device code of the library as assembly text (same flags as build())."""
     flags = [f for f in FLAGS if f not in ("-shared", "-fPIC")]
-    cmd = [HIPCC, *flags, "-S", "--cuda-device-only", "-o", "-", *SOURCES]
-    return subprocess.run(cmd, check=True, capture_output=True, text=True).stdout
+    return "".join(subprocess.run([HIPCC, *flags, "-S", "--cuda-device-only", "-o", "-", source],
+                                  check=True, capture_output=True, text=True).stdout
+                   for source in SOURCES)
 
 
 def ensure_built() -> str:

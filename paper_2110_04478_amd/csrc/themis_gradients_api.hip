@@ -1,0 +1,251 @@
+// C ABI of the gradient operators (see include/themis.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <tuple>
+#include <utility>
+
+#include "themis.h"
+#include "themis_elements.hpp"
+#include "themis_embedding.hpp"
+#include "themis_gradient.hpp"
+
+namespace themis {
+namespace {
+
+constexpr uint64_t kMost = 0x7fffffffu;   // of tokens, table rows and elements of a row
+constexpr uint64_t kMostTensors = 1u << 24;
+
+// Launches and keeps the first error that a launch of this call returns.
+struct Launches {
+  hipStream_t stream;
+  hipError_t first = hipSuccess;
+  explicit Launches(void* s) : stream((hipStream_t)s) {}
+  template <typename... P, typename... A>
+  void operator()(void (*kernel)(P...), dim3 grid, unsigned threads, A&&... a) {
+    std::tuple<P...> params(std::forward<A>(a)...);
+    launch(kernel, grid, threads, params, std::index_sequence_for<P...>{});
+  }
+  int status() const { return first == hipSuccess ? THEMIS_OK : THEMIS_ERR_DEVICE; }
+
+ private:
+  template <typename... P, size_t... I>
+  void launch(void (*kernel)(P...), dim3 grid, unsigned threads, std::tuple<P...>& params, std::index_sequence<I...>) {
+    if (first != hipSuccess) return;   // (what follows would work on what is not there)
+    void* ptrs[sizeof...(P)] = {(void*)&std::get<I>(params)...};
+    first = hipLaunchKernel((const void*)kernel, grid, dim3(threads), ptrs, 0, stream);
+  }
+};
+
+bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+// Rows that are only read.
+bool rows_ok(const themis_rows_t* r, bool index) {
+  return r && r->data && r->inner >= 1 && (index ? is_index_type(r->type) : is_float_type(r->type)) &&
+         aligned(r->data, type_bytes(r->type));
+}
+
+// Whether n rows of `width` elements share no element: the level with the shorter steps steps over
+// a row, the other over all of the shorter one's.
+bool rows_apart(const themis_rows_t& r, uint64_t n, uint64_t width) {
+  const uint64_t inner = std::min(r.inner, n), outer = (n + r.inner - 1) / r.inner;
+  struct Level { uint64_t count; __int128 stride; } a{inner, r.inner_stride}, b{outer, r.outer_stride};
+  if (a.stride < 0) a.stride = -a.stride;
+  if (b.stride < 0) b.stride = -b.stride;
+  if (a.count < 2) std::swap(a, b);
+  if (a.count < 2) return true;                            // one row
+  if (b.count < 2) return a.stride >= (__int128)width;
+  if (a.stride > b.stride) std::swap(a, b);
+  return a.stride >= (__int128)width && b.stride >= a.stride * (__int128)(a.count - 1) + (__int128)width;
+}
+
+uint32_t next_power(uint32_t x) {   // the smallest p with 2^p >= x
+  uint32_t p = 0;
+  while ((1u << p) < x) ++p;
+  return p;
+}
+
+}  // namespace
+}  // namespace themis
+
+using namespace themis;
+
+extern "C" {
+
+int themis_embedding_lookup(const themis_rows_t* table, uint64_t vocab, uint64_t width, const themis_rows_t* ids,
+                            uint64_t n, float scale, const themis_rows_t* out, void* stream) {
+  if (n == 0 || width == 0) return THEMIS_OK;
+  if (!rows_ok(ids, true) || !rows_ok(out, false)) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (!table || !is_float_type(table->type) || (vocab && !rows_ok(table, false))) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (n > kMost || width > kMost || vocab > kMost) return THEMIS_ERR_UNSUPPORTED;
+  if (!rows_apart(*out, n, width)) return THEMIS_ERR_INVALID_ARGUMENT;
+  const uint32_t vecs = (uint32_t)((width + kVec - 1) / kVec);
+  const uint32_t shift = std::min(next_power(vecs), 8u), chunks = (vecs + 255) / 256;
+  if (chunks > 65535) return THEMIS_ERR_UNSUPPORTED;
+  Launches go(stream);
+  auto run = [&](auto kernel, uint32_t rows) {
+    const uint64_t step = (256u >> shift) * rows;
+    const uint32_t blocks = (uint32_t)std::min<uint64_t>((n + step - 1) / step, 1u << 20);
+    go(kernel, dim3(blocks, chunks), 256, *table, (uint32_t)vocab, (uint32_t)width, *ids, (uint32_t)n, scale, *out,
+       shift);
+  };
+  with_type(table->type, [&](auto in) {
+    with_type(out->type, [&](auto to) { run(lookup_kernel<decltype(in), decltype(to), 1>, 1); });
+  });
+  return go.status();
+}
+
+size_t themis_embedding_grad_workspace_bytes(uint64_t n, uint64_t width, uint64_t vocab) {
+  (void)n, (void)width, (void)vocab;
+  return 0;
+}
+
+int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const themis_rows_t* ids, uint64_t n,
+                          float scale, int64_t ignored, int accumulate, const themis_rows_t* grad, uint64_t vocab,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  if (width == 0 || vocab == 0 || (n == 0 && accumulate)) return THEMIS_OK;
+  if (!rows_ok(grad, false)) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (n && (!rows_ok(ids, true) || !rows_ok(grad_out, false))) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (n > kMost || width > kMost || vocab > kMost) return THEMIS_ERR_UNSUPPORTED;
+  if (!rows_apart(*grad, vocab, width)) return THEMIS_ERR_INVALID_ARGUMENT;
+  const uint64_t need = themis_embedding_grad_workspace_bytes(n, width, vocab);
+  if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return THEMIS_ERR_WORKSPACE;
+  const uint64_t slabs = (width + 511) / 512;
+  if (slabs > 65535) return THEMIS_ERR_UNSUPPORTED;
+  const themis_rows_t none = {nullptr, THEMIS_F32, 1, 0, 0};
+  const uint32_t skip = ignored >= 0 && (uint64_t)ignored < vocab ? (uint32_t)ignored : ~0u;
+  Launches go(stream);
+  with_type(n ? grad_out->type : THEMIS_F32, [&](auto in) {
+    with_type(grad->type, [&](auto to) {
+      go(embedding_grad_kernel<decltype(in), decltype(to)>, dim3((uint32_t)std::min<uint64_t>(vocab, 1u << 20), slabs),
+         64, n ? *grad_out : none, (uint32_t)width, n ? *ids : none, (uint32_t)n, scale, skip, accumulate != 0, *grad,
+         (uint32_t)vocab);
+    });
+  });
+  return go.status();
+}
+
+int themis_gradient_plan(const themis_gradient_t* parts, uint64_t n_parts, uint64_t n_tensors,
+                         themis_gradient_plan_t* plan, void* image, size_t image_bytes) {
+  if (!plan || (n_parts && !parts)) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (n_tensors > kMostTensors) return THEMIS_ERR_UNSUPPORTED;
+  unsigned __int128 total = 0;
+  bool has_out = true, strided = false;
+  for (uint64_t i = 0; i < n_parts; ++i) {
+    const themis_gradient_t& g = parts[i];
+    if (g.tensor >= n_tensors || (i && g.tensor < parts[i - 1].tensor)) return THEMIS_ERR_INVALID_ARGUMENT;
+    if (!is_float_type(g.in_type) || (g.out && !is_float_type(g.out_type))) return THEMIS_ERR_INVALID_ARGUMENT;
+    const unsigned __int128 count = (unsigned __int128)g.rows * g.cols;
+    if (!count) continue;
+    if (!g.in || !aligned(g.in, type_bytes(g.in_type))) return THEMIS_ERR_INVALID_ARGUMENT;
+    if (g.out && !aligned(g.out, type_bytes(g.out_type))) return THEMIS_ERR_INVALID_ARGUMENT;
+    if (g.out == g.in && (g.in_type != g.out_type || g.in_row_stride != g.out_row_stride ||
+                          g.in_col_stride != g.out_col_stride)) return THEMIS_ERR_INVALID_ARGUMENT;
+    if (count >> 46) return THEMIS_ERR_UNSUPPORTED;
+    if (g.out && !rows_apart({g.out, g.out_type, g.cols, g.out_row_stride, g.out_col_stride}, (uint64_t)count, 1))
+      return THEMIS_ERR_INVALID_ARGUMENT;   // (an element written twice)
+    has_out = has_out && g.out;
+    total += count;
+  }
+  if (total >> 46) return THEMIS_ERR_UNSUPPORTED;
+  // Pieces: small where the list is, so that it reaches all CUs, and of one size in multiples of
+  // what a workgroup takes at a time.
+  uint64_t most = ((uint64_t)total / (2 * kNormGroups) + kPieceLeast - 1) / kPieceLeast * kPieceLeast;
+  most = std::min<uint64_t>(std::max<uint64_t>(most, kPieceLeast), kPieceMost);
+
+  uint64_t n_pieces = 0;
+  Piece* to = (Piece*)image;
+  uint64_t room = 0;
+  uint32_t* first = nullptr;
+  auto walk = [&](bool write) {
+    uint64_t at = 0, tensor = 0;
+    for (uint64_t i = 0; i < n_parts; ++i) {
+      const themis_gradient_t& g = parts[i];
+      for (; write && tensor <= g.tensor; ++tensor) first[tensor] = (uint32_t)at;
+      uint64_t rows = g.rows, cols = g.cols;
+      if (!rows || !cols) continue;
+      const bool in_run = rows == 1 || (g.in_row_stride == (int64_t)cols && g.in_col_stride == 1);
+      const bool out_run = !g.out || rows == 1 || (g.out_row_stride == (int64_t)cols && g.out_col_stride == 1);
+      if (in_run && out_run) { cols *= rows; rows = 1; }   // one row, each with its one stride
+      strided = strided || rows > 1 || (cols > 1 && (g.in_col_stride != 1 || (g.out && g.out_col_stride != 1)));
+      const uint64_t wide = std::min(cols, most), high = std::max<uint64_t>(most / wide, 1);
+      for (uint64_t r = 0; r < rows; r += high)
+        for (uint64_t c = 0; c < cols; c += wide, ++at) {
+          if (!write) continue;
+          Piece p;
+          const uint64_t nr = std::min(high, rows - r), nc = std::min(wide, cols - c);
+          const int64_t in_at = (int64_t)r * g.in_row_stride + (int64_t)c * g.in_col_stride;
+          const int64_t out_at = (int64_t)r * g.out_row_stride + (int64_t)c * g.out_col_stride;
+          p.in = (const char*)g.in + in_at * type_bytes(g.in_type);
+          p.out = g.out ? (char*)g.out + out_at * type_bytes(g.out_type) : nullptr;
+          p.count = (uint32_t)(nr * nc);
+          p.cols = (uint32_t)nc;
+          p.tensor = g.tensor;
+          const bool one = nr == 1 || nc == cols;
+          const bool in_dense = (g.in_col_stride == 1 || nc == 1) && (nr == 1 || (one && g.in_row_stride == (int64_t)nc));
+          const bool out_dense = (g.out_col_stride == 1 || nc == 1) && (nr == 1 || (one && g.out_row_stride == (int64_t)nc));
+          p.kind = (uint32_t)g.in_type | (uint32_t)(g.out ? g.out_type : 0) << 8 | (in_dense ? kInDense : 0) |
+                   (out_dense ? kOutDense : 0) | (g.out == g.in ? kInPlace : 0);
+          p.in_row = g.in_row_stride;
+          p.in_col = g.in_col_stride;
+          p.out_row = g.out_row_stride;
+          p.out_col = g.out_col_stride;
+          to[at] = p;
+        }
+    }
+    for (; write && tensor <= n_tensors; ++tensor) first[tensor] = (uint32_t)at;
+    n_pieces = at;
+  };
+  walk(false);
+  if (n_pieces >= kMost) return THEMIS_ERR_UNSUPPORTED;
+  room = n_pieces * sizeof(Piece) + (n_tensors + 1) * sizeof(uint32_t);
+  plan->n_tensors = n_tensors;
+  plan->n_pieces = n_pieces;
+  plan->image_bytes = room;
+  plan->workspace_bytes = (norm_groups((uint32_t)n_pieces) + n_pieces) * sizeof(double);
+  plan->has_out = has_out;
+  plan->strided = strided;
+  plan->image = nullptr;
+  if (!image) return THEMIS_OK;
+  if (image_bytes < room || !aligned(image, 8)) return THEMIS_ERR_WORKSPACE;
+  first = (uint32_t*)(to + n_pieces);
+  walk(true);
+  return THEMIS_OK;
+}
+
+static int gradient_pass(const themis_gradient_plan_t* plan, double max_norm, bool clip, float* total, float* norms,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  if (!plan || !plan->image || !total || !aligned(plan->image, 16)) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (plan->n_pieces >= kMost || plan->n_tensors > kMostTensors) return THEMIS_ERR_UNSUPPORTED;
+  if (clip && (!(max_norm > 0.0) || !std::isfinite(max_norm) || !plan->has_out)) return THEMIS_ERR_INVALID_ARGUMENT;
+  const uint32_t groups = norm_groups((uint32_t)plan->n_pieces);
+  const size_t need = (groups + plan->n_pieces) * sizeof(double);
+  if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return THEMIS_ERR_WORKSPACE;
+  const PlanView view = plan_view(*plan);
+  double* group_sums = (double*)workspace;
+  double* piece_sums = group_sums + groups;
+  const uint32_t norm_blocks = norms ? (uint32_t)((plan->n_tensors + 3) / 4) : 0u;
+  Launches go(stream);
+  if (groups) go(norm_kernel, dim3(groups), 256, view, group_sums, piece_sums);
+  if (clip) {
+    const uint32_t scalers = std::max(groups, 1u);
+    go(clip_kernel, dim3(scalers + norm_blocks), 256, view, groups, group_sums, piece_sums, max_norm, scalers, total,
+       norms);
+  } else {
+    go(norm_finish_kernel, dim3(1 + norm_blocks), 256, view, groups, group_sums, piece_sums, total, norms);
+  }
+  return go.status();
+}
+
+int themis_gradient_norm(const themis_gradient_plan_t* plan, float* total, float* norms, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  return gradient_pass(plan, 1.0, false, total, norms, workspace, workspace_bytes, stream);
+}
+
+int themis_gradient_clip(const themis_gradient_plan_t* plan, double max_norm, float* total, float* norms,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  return gradient_pass(plan, max_norm, true, total, norms, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"
