@@ -48,33 +48,264 @@ lookup_kernel(themis_rows_t table, uint32_t vocab, uint32_t width, themis_rows_t
 // ---------------------------------------------------------------------------
 // themis_embedding_grad: grad[v] (+)= scale * sum of grad_out[t] over ids[t] == v.
 //
-// A wavefront per table row and 512 of its elements: it looks through all token numbers, 64 at a
-// time, and adds the rows of those that are its own in ascending order.
+// The tokens are sorted by their number, stable, so that a table row's tokens stand next to each
+// other in ascending order; the sorted list is cut into tiles of one length, whatever the numbers
+// are, so that a token that makes up half of the list costs no more than any other half.  A tile
+// adds its rows one after the other and writes the sums that begin and end in it.  A sum that
+// crosses tiles is left in parts, which are added in the order of the tiles.
+//
+// Sort: least significant digit first, up to ten bits a pass and two launches: every workgroup
+// counts the digits of its part of the list, then every workgroup finds from all counts where its
+// part's tokens go.  A token's key is its number, or `vocab` (behind all others) if it has no
+// gradient.
 // ---------------------------------------------------------------------------
-template <typename In, typename Out>
-__global__ void __launch_bounds__(64)
-embedding_grad_kernel(themis_rows_t grad_out, uint32_t width, themis_rows_t ids, uint32_t n, float scale,
-                      uint32_t ignored, bool accumulate, themis_rows_t grad, uint32_t vocab) {
-  const uint32_t col = (blockIdx.y * 64u + threadIdx.x) * kVec;
-  const uint32_t count = col < width ? min(width - col, (uint32_t)kVec) : 0u;
-  for (uint32_t v = blockIdx.x; v < vocab; v += gridDim.x) {
-    float8 sum = 0.0f;
-    bool any = false;
-    for (uint32_t t = 0; t < n; t += 64) {
-      const uint32_t id = t + threadIdx.x < n ? token_row(ids, t + threadIdx.x, vocab) : ~0u;
-      uint64_t mine = v == ignored ? 0ull : __ballot(id == v);
-      any |= mine != 0;
-      for (; mine; mine &= mine - 1) {
-        const uint32_t at = t + (uint32_t)__builtin_ctzll(mine);
-        if (count) sum += widen8<In>(load_some((const In*)grad_out.data + row_offset(grad_out, at) + col, count));
-      }
-    }
-    if (!count || (accumulate && !any)) continue;
-    Out* to = (Out*)grad.data + row_offset(grad, v) + col;
-    float8 x = sum * scale;
-    if (accumulate) x = widen8<Out>(load_some(to, count)) + x;
-    store_some(to, x, count);
+constexpr uint32_t kMaxBins = 1024;
+constexpr uint32_t kSortGroup = 256, kSortWaves = kSortGroup / 64;
+
+struct SortView {
+  uint32_t n, part;      // tokens, tokens of a workgroup (a multiple of kSortGroup)
+  uint32_t parts;        // workgroups
+  uint32_t shift, bits;  // the pass's digit
+  uint32_t* counts;      // [parts][1 << bits]
+  const uint32_t* key_in;    // the pass before's, or none: the token numbers themselves
+  const uint32_t* token_in;
+  uint32_t* key_out;
+  uint32_t* token_out;
+};
+
+__device__ __forceinline__ uint32_t sort_key(const SortView& s, const themis_rows_t& ids, uint32_t vocab,
+                                             uint32_t ignored, uint32_t i) {
+  if (s.key_in) return s.key_in[i];
+  const uint32_t id = token_row(ids, i, vocab);
+  return id == ~0u || id == ignored ? vocab : id;
+}
+
+__global__ void __launch_bounds__(kSortGroup)
+sort_count_kernel(SortView s, themis_rows_t ids, uint32_t vocab, uint32_t ignored) {
+  __shared__ uint32_t count[kMaxBins];
+  const uint32_t bins = 1u << s.bits, first = blockIdx.x * s.part;
+  const uint32_t last = min(first + s.part, s.n);
+  for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) count[b] = 0;
+  __syncthreads();
+  for (uint32_t i = first + threadIdx.x; i < last; i += kSortGroup)
+    atomicAdd(&count[(sort_key(s, ids, vocab, ignored, i) >> s.shift) & (bins - 1)], 1u);
+  __syncthreads();
+  for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) s.counts[blockIdx.x * bins + b] = count[b];
+}
+
+// The sum of x over the lanes before this one, of a workgroup of kSortGroup.
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t (&wave_sums)[kSortWaves]) {
+  uint32_t upto = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t y = __shfl_up(upto, d);
+    if ((threadIdx.x & 63u) >= (uint32_t)d) upto += y;
   }
+  if ((threadIdx.x & 63u) == 63) wave_sums[threadIdx.x >> 6] = upto;
+  __syncthreads();
+  for (uint32_t w = 0; w < (threadIdx.x >> 6); ++w) upto += wave_sums[w];
+  return upto - x;
+}
+
+__global__ void __launch_bounds__(kSortGroup)
+sort_move_kernel(SortView s, themis_rows_t ids, uint32_t vocab, uint32_t ignored) {
+  __shared__ uint32_t place[kSortWaves][kMaxBins];   // first a wavefront's counts, then where its next one goes
+  __shared__ uint32_t wave_sums[kSortWaves];
+  const uint32_t bins = 1u << s.bits, first = blockIdx.x * s.part;
+  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
+  const uint32_t share = s.part / kSortWaves;   // a wavefront's tokens stand together (a multiple of 64)
+  const uint32_t begin = min(first + wave * share, s.n), end = min(begin + share, s.n);
+  for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup)
+#pragma unroll
+    for (uint32_t w = 0; w < kSortWaves; ++w) place[w][b] = 0;
+  __syncthreads();
+  for (uint32_t i = begin + lane; i < end; i += 64)
+    atomicAdd(&place[wave][(sort_key(s, ids, vocab, ignored, i) >> s.shift) & (bins - 1)], 1u);
+  // Where a digit's tokens of this part go: behind all of smaller digits and those of the parts before.
+  const uint32_t per = (bins + kSortGroup - 1) / kSortGroup;   // 1..4 adjacent digits of a lane
+  uint32_t before[kMaxBins / kSortGroup], all = 0;
+#pragma unroll
+  for (uint32_t k = 0; k < kMaxBins / kSortGroup; ++k) {
+    const uint32_t b = threadIdx.x * per + k;
+    before[k] = 0;
+    if (k >= per || b >= bins) continue;
+    uint32_t mine = 0, total = 0;
+    for (uint32_t p = 0; p < s.parts; ++p) {
+      const uint32_t c = s.counts[p * bins + b];
+      mine += p < blockIdx.x ? c : 0u;
+      total += c;
+    }
+    before[k] = all + mine;
+    all += total;
+  }
+  const uint32_t base = sum_before(all, wave_sums);   // (a barrier: the counts above are complete)
+#pragma unroll
+  for (uint32_t k = 0; k < kMaxBins / kSortGroup; ++k) {
+    const uint32_t b = threadIdx.x * per + k;
+    if (k >= per || b >= bins) continue;
+    uint32_t at = base + before[k];
+#pragma unroll
+    for (uint32_t w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = place[w][b];
+      place[w][b] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  for (uint32_t i0 = begin; i0 < end; i0 += 64) {
+    const uint32_t i = i0 + lane;
+    const bool on = i < end;
+    const uint32_t key = on ? sort_key(s, ids, vocab, ignored, i) : 0u;
+    const uint32_t token = on ? (s.key_in ? s.token_in[i] : i) : 0u;
+    const uint32_t digit = (key >> s.shift) & (bins - 1);
+    uint64_t same = __ballot(on);   // lanes with this lane's digit
+    for (uint32_t b = 0; b < s.bits; ++b) {
+      const uint64_t ones = __ballot((digit >> b) & 1u);
+      same &= (digit >> b) & 1u ? ones : ~ones;
+    }
+    const uint32_t rank = (uint32_t)__popcll(same & ((1ull << lane) - 1));
+    // (all lanes have read before the first of a digit's adds: a wavefront's accesses to LDS are
+    // served in the order of the program, and these are kept in it)
+    const uint32_t at = (on ? __hip_atomic_load(&place[wave][digit], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0u) + rank;
+    if (on && rank == 0)
+      __hip_atomic_store(&place[wave][digit], at + (uint32_t)__popcll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    if (on) {
+      s.key_out[at] = key;
+      s.token_out[at] = token;
+    }
+  }
+}
+
+// The sorted list in tiles.
+struct TileView {
+  const uint32_t* key;     // [n], ascending, rounded up to a multiple of kTileStep
+  const uint32_t* token;
+  uint32_t n, tile;        // tokens, tokens of a tile (a multiple of kTileStep)
+  uint32_t tiles, slabs;   // slabs of 512 elements
+  uint32_t shift;          // 2^shift lanes take a tile's slab (less than 64 where the rows are short)
+  uint32_t tile_groups;    // workgroups that take tiles; the others write zeros
+  uint32_t fill_rows;      // table rows of one of those, up to 64
+  float* parts;            // [tiles][2][stride]: of a sum that began before, of one that goes on
+  uint32_t stride;
+};
+constexpr uint32_t kTileStep = 8;   // rows in flight
+
+// Zeros in those of up to 64 table rows from `v0` on that no token has: a lane looks for its row.
+template <typename Out>
+__device__ __forceinline__ void fill_rows(const TileView& s, uint32_t v0, uint32_t width, const themis_rows_t& grad,
+                                          uint32_t vocab) {
+  const uint32_t lane = threadIdx.x & 63u, v = v0 + lane;
+  const bool mine = lane < s.fill_rows && v < vocab;
+  uint32_t lo = 0, hi = mine ? s.n : 0u;   // the first key that is not smaller
+  while (__any(lo < hi)) {
+    if (lo < hi) {
+      const uint32_t mid = lo + ((hi - lo) >> 1);
+      if (s.key[mid] < v) lo = mid + 1;
+      else hi = mid;
+    }
+  }
+  uint64_t empty = __ballot(mine && (lo >= s.n || s.key[lo] != v));
+  const uint32_t vecs = (width + kVec - 1) / kVec;
+  const float8 zero = 0.0f;
+  for (; empty; empty &= empty - 1) {
+    Out* to = (Out*)grad.data + row_offset(grad, v0 + (uint32_t)__builtin_ctzll(empty));
+    for (uint32_t c = threadIdx.x; c < vecs; c += 256) store_some(to + c * kVec, zero, min(width - c * kVec, (uint32_t)kVec));
+  }
+}
+
+template <typename Out>
+__device__ __forceinline__ void write_sum(const themis_rows_t& grad, uint32_t v, uint32_t col, uint32_t count,
+                                          float8 sum, float scale, bool accumulate) {
+  Out* to = (Out*)grad.data + row_offset(grad, v) + col;
+  float8 x = sum * scale;
+  if (accumulate) x = widen8<Out>(load_some(to, count)) + x;
+  store_some(to, x, count);
+}
+
+template <typename In, typename Out>
+__global__ void __launch_bounds__(256)
+tile_sum_kernel(TileView s, themis_rows_t grad_out, uint32_t width, float scale, bool accumulate, themis_rows_t grad,
+                uint32_t vocab) {
+  if (blockIdx.x >= s.tile_groups) {
+    const uint64_t step = (uint64_t)(gridDim.x - s.tile_groups) * s.fill_rows;
+    for (uint64_t v = (uint64_t)(blockIdx.x - s.tile_groups) * s.fill_rows; v < vocab; v += step)
+      fill_rows<Out>(s, (uint32_t)v, width, grad, vocab);
+    return;
+  }
+  const uint32_t item = blockIdx.x * (256u >> s.shift) + (threadIdx.x >> s.shift);
+  const uint32_t tile = item / s.slabs, slab = item - tile * s.slabs;
+  const uint32_t col = (slab * 64u + (threadIdx.x & ((1u << s.shift) - 1u))) * kVec;
+  if (tile >= s.tiles || col >= width) return;
+  const uint32_t count = min(width - col, (uint32_t)kVec);
+  const uint32_t first = tile * s.tile, last = min(first + s.tile, s.n);
+  bool head = first > 0 && s.key[first - 1] == s.key[first];
+  float8 sum = 0.0f;
+  for (uint32_t j = first; j < last; j += kTileStep) {
+    uint32_t key[kTileStep + 1], token[kTileStep];
+#pragma unroll
+    for (uint32_t u = 0; u < kTileStep; ++u) {
+      key[u] = s.key[j + u];
+      token[u] = s.token[j + u];
+    }
+    key[kTileStep] = j + kTileStep < s.n ? s.key[j + kTileStep] : ~0u;
+    if (key[0] >= vocab) break;
+    typename Packed<In>::type v[kTileStep];
+#pragma unroll
+    for (uint32_t u = 0; u < kTileStep; ++u)
+      if (j + u < last && key[u] < vocab)
+        v[u] = load_some((const In*)grad_out.data + row_offset(grad_out, token[u]) + col, count);
+#pragma unroll
+    for (uint32_t u = 0; u < kTileStep; ++u) {
+      if (j + u >= last || key[u] >= vocab) break;
+      sum += widen8<In>(v[u]);
+      const bool goes_on = j + u + 1 < s.n && key[u + 1] == key[u];
+      if (goes_on && j + u + 1 < last) continue;
+      if (head || goes_on) {
+        float* to = s.parts + ((uint64_t)tile * 2 + (head ? 0 : 1)) * s.stride + col;
+        store8(to, sum);
+      } else {
+        write_sum<Out>(grad, key[u], col, count, sum, scale, accumulate);
+      }
+      head = false;
+      sum = 0.0f;
+    }
+  }
+}
+
+// Adds the parts of a sum that crosses tiles: a workgroup for every tile in which one begins and
+// does not end, its four wavefronts a quarter of the parts each.
+template <typename Out>
+__global__ void __launch_bounds__(256)
+tile_join_kernel(TileView s, uint32_t width, float scale, bool accumulate, themis_rows_t grad, uint32_t vocab) {
+  __shared__ float8 quarter[3][64];
+  const uint32_t tile = blockIdx.x, first = tile * s.tile, next = first + s.tile;
+  if (next >= s.n) return;
+  const uint32_t v = s.key[next - 1];
+  if (v >= vocab || s.key[next] != v) return;
+  if (first > 0 && s.key[first - 1] == v) return;   // it began before
+  uint32_t lo = next, hi = s.n;   // where it ends
+  while (lo < hi) {
+    const uint32_t mid = lo + ((hi - lo) >> 1);
+    if (s.key[mid] <= v) lo = mid + 1;
+    else hi = mid;
+  }
+  const uint32_t more = (lo - 1) / s.tile - tile;   // parts behind the first
+  const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
+  const uint32_t col = (blockIdx.y * 64u + lane) * kVec;
+  const bool on = col < width;
+  const uint32_t each = (more + 1 + 3) / 4, begin = min(wave * each, more + 1), end = min(begin + each, more + 1);
+  float8 sum = 0.0f;
+  if (on) {
+#pragma unroll 8
+    for (uint32_t p = begin; p < end; ++p)
+      sum += load8(s.parts + ((uint64_t)(tile + p) * 2 + (p == 0 ? 1 : 0)) * s.stride + col);
+  }
+  if (wave) quarter[wave - 1][lane] = sum;
+  __syncthreads();
+  if (wave || !on) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) sum += quarter[w][lane];
+  write_sum<Out>(grad, v, col, min(width - col, (uint32_t)kVec), sum, scale, accumulate);
 }
 
 }  // namespace themis

@@ -66,6 +66,47 @@ uint32_t next_power(uint32_t x) {   // the smallest p with 2^p >= x
   return p;
 }
 
+// How a gradient of the table is worked out, and what is where in its workspace (bytes).
+struct GradLayout {
+  uint32_t passes, bits;           // of the sort
+  uint32_t part, sort_parts;       // tokens of a workgroup, workgroups
+  uint32_t tile, tiles, slabs, shift, stride;
+  size_t key[2], token[2], counts, parts, bytes;
+};
+
+GradLayout grad_layout(uint32_t n, uint32_t width, uint32_t vocab) {
+  GradLayout l = {};
+  if (n == 0) return l;
+  const uint32_t bits = next_power(vocab + 1);   // keys 0 .. vocab
+  l.passes = (bits + 9) / 10;
+  l.bits = (bits + l.passes - 1) / l.passes;
+  l.part = std::max(1024u, (uint32_t)(((uint64_t)n + 255) / 256 + kSortGroup - 1) / kSortGroup * kSortGroup);
+  l.sort_parts = (n + l.part - 1) / l.part;
+  const uint32_t vecs = (width + kVec - 1) / kVec;
+  l.shift = std::min(next_power(vecs), 6u);
+  l.slabs = (vecs + 63) / 64;
+  l.stride = l.slabs * 512;
+  // Tiles: long, so that few sums cross one, as long as there is a wavefront for every SIMD four times.
+  l.tile = 128;
+  while (l.tile > 16 && (((uint64_t)n + l.tile - 1) / l.tile * l.slabs << l.shift) / 64 < 4096) l.tile /= 2;
+  l.tiles = (n + l.tile - 1) / l.tile;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) / 256 * 256;
+    return here;
+  };
+  const size_t list = ((size_t)n + kTileStep) * sizeof(uint32_t);
+  for (int k = 0; k < (l.passes > 1 ? 2 : 1); ++k) {
+    l.key[k] = take(list);
+    l.token[k] = take(list);
+  }
+  l.counts = take((size_t)l.sort_parts * (sizeof(uint32_t) << l.bits));
+  l.parts = take((size_t)l.tiles * 2 * l.stride * sizeof(float));
+  l.bytes = at;
+  return l;
+}
+
 }  // namespace
 }  // namespace themis
 
@@ -97,8 +138,8 @@ int themis_embedding_lookup(const themis_rows_t* table, uint64_t vocab, uint64_t
 }
 
 size_t themis_embedding_grad_workspace_bytes(uint64_t n, uint64_t width, uint64_t vocab) {
-  (void)n, (void)width, (void)vocab;
-  return 0;
+  if (n == 0 || width == 0 || vocab == 0 || n > kMost || width > kMost || vocab > kMost) return 0;
+  return grad_layout((uint32_t)n, (uint32_t)width, (uint32_t)vocab).bytes;
 }
 
 int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const themis_rows_t* ids, uint64_t n,
@@ -109,20 +150,58 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
   if (n && (!rows_ok(ids, true) || !rows_ok(grad_out, false))) return THEMIS_ERR_INVALID_ARGUMENT;
   if (n > kMost || width > kMost || vocab > kMost) return THEMIS_ERR_UNSUPPORTED;
   if (!rows_apart(*grad, vocab, width)) return THEMIS_ERR_INVALID_ARGUMENT;
-  const uint64_t need = themis_embedding_grad_workspace_bytes(n, width, vocab);
-  if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return THEMIS_ERR_WORKSPACE;
-  const uint64_t slabs = (width + 511) / 512;
-  if (slabs > 65535) return THEMIS_ERR_UNSUPPORTED;
+  const GradLayout l = grad_layout((uint32_t)n, (uint32_t)width, (uint32_t)vocab);
+  if (l.bytes && (!workspace || workspace_bytes < l.bytes || !aligned(workspace, 16))) return THEMIS_ERR_WORKSPACE;
+  const uint64_t items = (uint64_t)l.tiles * l.slabs, per_group = 256u >> l.shift;
+  const uint64_t tile_groups = (items + per_group - 1) / per_group;
+  if (tile_groups > 1u << 23 || l.slabs > 65535) return THEMIS_ERR_UNSUPPORTED;   // (grids of less than 2^32 lanes)
   const themis_rows_t none = {nullptr, THEMIS_F32, 1, 0, 0};
+  const themis_rows_t g = n ? *grad_out : none, k = n ? *ids : none;
   const uint32_t skip = ignored >= 0 && (uint64_t)ignored < vocab ? (uint32_t)ignored : ~0u;
   Launches go(stream);
-  with_type(n ? grad_out->type : THEMIS_F32, [&](auto in) {
+  char* at = (char*)workspace;
+  uint32_t *key[2] = {(uint32_t*)(at + l.key[0]), (uint32_t*)(at + l.key[1])};
+  uint32_t *token[2] = {(uint32_t*)(at + l.token[0]), (uint32_t*)(at + l.token[1])};
+  for (uint32_t pass = 0; pass < l.passes && n; ++pass) {
+    SortView s;
+    s.n = (uint32_t)n;
+    s.part = l.part;
+    s.parts = l.sort_parts;
+    s.shift = pass * l.bits;
+    s.bits = l.bits;
+    s.counts = (uint32_t*)(at + l.counts);
+    s.key_in = pass ? key[(pass - 1) & 1] : nullptr;
+    s.token_in = pass ? token[(pass - 1) & 1] : nullptr;
+    s.key_out = key[pass & 1];
+    s.token_out = token[pass & 1];
+    go(sort_count_kernel, dim3(s.parts), kSortGroup, s, k, (uint32_t)vocab, skip);
+    go(sort_move_kernel, dim3(s.parts), kSortGroup, s, k, (uint32_t)vocab, skip);
+  }
+  TileView t;
+  t.key = key[(l.passes - 1) & 1];
+  t.token = token[(l.passes - 1) & 1];
+  t.n = (uint32_t)n;
+  t.tile = l.tile;
+  t.tiles = l.tiles;
+  t.slabs = l.slabs;
+  t.shift = l.shift;
+  t.parts = (float*)(at + l.parts);
+  t.stride = l.stride;
+  t.tile_groups = (uint32_t)tile_groups;
+  // (a workgroup's zeros: about 256 KiB, in up to 64 rows)
+  t.fill_rows = (uint32_t)std::min<uint64_t>(64, std::max<uint64_t>(1, (256u << 10) / (width * type_bytes(grad->type))));
+  const uint64_t fill = accumulate ? 0 : std::min<uint64_t>((vocab + t.fill_rows - 1) / t.fill_rows, 1u << 20);
+  with_type(g.type, [&](auto in) {
     with_type(grad->type, [&](auto to) {
-      go(embedding_grad_kernel<decltype(in), decltype(to)>, dim3((uint32_t)std::min<uint64_t>(vocab, 1u << 20), slabs),
-         64, n ? *grad_out : none, (uint32_t)width, n ? *ids : none, (uint32_t)n, scale, skip, accumulate != 0, *grad,
-         (uint32_t)vocab);
+      go(tile_sum_kernel<decltype(in), decltype(to)>, dim3(t.tile_groups + (uint32_t)fill), 256, t, g, (uint32_t)width,
+         scale, accumulate != 0, *grad, (uint32_t)vocab);
     });
   });
+  if (l.tiles > 1)
+    with_type(grad->type, [&](auto to) {
+      go(tile_join_kernel<decltype(to)>, dim3(l.tiles - 1, l.slabs), 256, t, (uint32_t)width, scale, accumulate != 0,
+         *grad, (uint32_t)vocab);
+    });
   return go.status();
 }
 
