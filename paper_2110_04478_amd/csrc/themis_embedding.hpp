@@ -60,7 +60,7 @@ lookup_kernel(themis_rows_t table, uint32_t vocab, uint32_t width, themis_rows_t
 // gradient.
 // ---------------------------------------------------------------------------
 constexpr uint32_t kMaxBins = 1024;
-constexpr uint32_t kSortGroup = 256, kSortWaves = kSortGroup / 64;
+constexpr uint32_t kSortGroup = 1024, kSortWaves = kSortGroup / 64;
 
 struct SortView {
   uint32_t n, part;      // tokens, tokens of a workgroup (a multiple of kSortGroup)
@@ -93,20 +93,6 @@ sort_count_kernel(SortView s, themis_rows_t ids, uint32_t vocab, uint32_t ignore
   for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) s.counts[blockIdx.x * bins + b] = count[b];
 }
 
-// The sum of x over the lanes before this one, of a workgroup of kSortGroup.
-__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t (&wave_sums)[kSortWaves]) {
-  uint32_t upto = x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t y = __shfl_up(upto, d);
-    if ((threadIdx.x & 63u) >= (uint32_t)d) upto += y;
-  }
-  if ((threadIdx.x & 63u) == 63) wave_sums[threadIdx.x >> 6] = upto;
-  __syncthreads();
-  for (uint32_t w = 0; w < (threadIdx.x >> 6); ++w) upto += wave_sums[w];
-  return upto - x;
-}
-
 __global__ void __launch_bounds__(kSortGroup)
 sort_move_kernel(SortView s, themis_rows_t ids, uint32_t vocab, uint32_t ignored) {
   __shared__ uint32_t place[kSortWaves][kMaxBins];   // first a wavefront's counts, then where its next one goes
@@ -115,42 +101,41 @@ sort_move_kernel(SortView s, themis_rows_t ids, uint32_t vocab, uint32_t ignored
   const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
   const uint32_t share = s.part / kSortWaves;   // a wavefront's tokens stand together (a multiple of 64)
   const uint32_t begin = min(first + wave * share, s.n), end = min(begin + share, s.n);
-  for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup)
+  const uint32_t b = threadIdx.x;               // a lane has one digit, or none
+  if (b < bins)
 #pragma unroll
     for (uint32_t w = 0; w < kSortWaves; ++w) place[w][b] = 0;
   __syncthreads();
   for (uint32_t i = begin + lane; i < end; i += 64)
     atomicAdd(&place[wave][(sort_key(s, ids, vocab, ignored, i) >> s.shift) & (bins - 1)], 1u);
   // Where a digit's tokens of this part go: behind all of smaller digits and those of the parts before.
-  const uint32_t per = (bins + kSortGroup - 1) / kSortGroup;   // 1..4 adjacent digits of a lane
-  uint32_t before[kMaxBins / kSortGroup], all = 0;
-#pragma unroll
-  for (uint32_t k = 0; k < kMaxBins / kSortGroup; ++k) {
-    const uint32_t b = threadIdx.x * per + k;
-    before[k] = 0;
-    if (k >= per || b >= bins) continue;
-    uint32_t mine = 0, total = 0;
+  uint32_t before = 0, all = 0;
+  if (b < bins) {
+#pragma unroll 8
     for (uint32_t p = 0; p < s.parts; ++p) {
       const uint32_t c = s.counts[p * bins + b];
-      mine += p < blockIdx.x ? c : 0u;
-      total += c;
+      before += p < blockIdx.x ? c : 0u;
+      all += c;
     }
-    before[k] = all + mine;
-    all += total;
   }
-  const uint32_t base = sum_before(all, wave_sums);   // (a barrier: the counts above are complete)
+  uint32_t upto = all;
 #pragma unroll
-  for (uint32_t k = 0; k < kMaxBins / kSortGroup; ++k) {
-    const uint32_t b = threadIdx.x * per + k;
-    if (k >= per || b >= bins) continue;
-    uint32_t at = base + before[k];
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t y = __shfl_up(upto, d);
+    if (lane >= (uint32_t)d) upto += y;
+  }
+  if (lane == 63) wave_sums[wave] = upto;
+  __syncthreads();   // (the counts in LDS are complete as well)
+  uint32_t at = upto - all + before;
+#pragma unroll
+  for (uint32_t w = 0; w < kSortWaves; ++w) at += w < wave ? wave_sums[w] : 0u;
+  if (b < bins)
 #pragma unroll
     for (uint32_t w = 0; w < kSortWaves; ++w) {
       const uint32_t c = place[w][b];
       place[w][b] = at;
       at += c;
     }
-  }
   __syncthreads();
   for (uint32_t i0 = begin; i0 < end; i0 += 64) {
     const uint32_t i = i0 + lane;
@@ -176,19 +161,21 @@ sort_move_kernel(SortView s, themis_rows_t ids, uint32_t vocab, uint32_t ignored
   }
 }
 
-// The sorted list in tiles.
+// The sorted list in tiles, one for every group of lanes of a workgroup (a wavefront, less where the
+// rows are short), and the tiles of a workgroup in blocks.
 struct TileView {
   const uint32_t* key;     // [n], ascending, rounded up to a multiple of kTileStep
   const uint32_t* token;
   uint32_t n, tile;        // tokens, tokens of a tile (a multiple of kTileStep)
-  uint32_t tiles, slabs;   // slabs of 512 elements
-  uint32_t shift;          // 2^shift lanes take a tile's slab (less than 64 where the rows are short)
-  uint32_t tile_groups;    // workgroups that take tiles; the others write zeros
-  uint32_t fill_rows;      // table rows of one of those, up to 64
-  float* parts;            // [tiles][2][stride]: of a sum that began before, of one that goes on
+  uint32_t block;          // tokens of a block
+  uint32_t blocks, slabs;  // slabs of 512 elements
+  uint32_t shift;          // 2^shift lanes take a tile's slab
+  uint32_t fill_rows;      // table rows of a workgroup that writes zeros, up to 64
+  float* parts;            // [blocks][2][stride]: of a sum that began before, of one that goes on
   uint32_t stride;
 };
-constexpr uint32_t kTileStep = 8;   // rows in flight
+constexpr uint32_t kTileStep = 8;    // rows in flight
+constexpr uint32_t kLeastShift = 3;  // (up to 32 groups of lanes)
 
 // Zeros in those of up to 64 table rows from `v0` on that no token has: a lane looks for its row.
 template <typename Out>
@@ -226,79 +213,114 @@ template <typename In, typename Out>
 __global__ void __launch_bounds__(256)
 tile_sum_kernel(TileView s, themis_rows_t grad_out, uint32_t width, float scale, bool accumulate, themis_rows_t grad,
                 uint32_t vocab) {
-  if (blockIdx.x >= s.tile_groups) {
-    const uint64_t step = (uint64_t)(gridDim.x - s.tile_groups) * s.fill_rows;
-    for (uint64_t v = (uint64_t)(blockIdx.x - s.tile_groups) * s.fill_rows; v < vocab; v += step)
+  // A group's sums that its tile does not hold whole: of one that began before, of one that goes on.
+  __shared__ float8 part[2][256];
+  const uint32_t sums = s.blocks * s.slabs;
+  if (blockIdx.x >= sums) {
+    const uint64_t step = (uint64_t)(gridDim.x - sums) * s.fill_rows;
+    for (uint64_t v = (uint64_t)(blockIdx.x - sums) * s.fill_rows; v < vocab; v += step)
       fill_rows<Out>(s, (uint32_t)v, width, grad, vocab);
     return;
   }
-  const uint32_t item = blockIdx.x * (256u >> s.shift) + (threadIdx.x >> s.shift);
-  const uint32_t tile = item / s.slabs, slab = item - tile * s.slabs;
-  const uint32_t col = (slab * 64u + (threadIdx.x & ((1u << s.shift) - 1u))) * kVec;
-  if (tile >= s.tiles || col >= width) return;
-  const uint32_t count = min(width - col, (uint32_t)kVec);
-  const uint32_t first = tile * s.tile, last = min(first + s.tile, s.n);
-  bool head = first > 0 && s.key[first - 1] == s.key[first];
-  float8 sum = 0.0f;
-  for (uint32_t j = first; j < last; j += kTileStep) {
-    uint32_t key[kTileStep + 1], token[kTileStep];
+  const uint32_t block = blockIdx.x / s.slabs, slab = blockIdx.x - block * s.slabs;
+  const uint32_t lanes = 1u << s.shift, group = threadIdx.x >> s.shift;
+  const uint32_t col = (slab * 64u + (threadIdx.x & (lanes - 1u))) * kVec;
+  const uint32_t count = col < width ? min(width - col, (uint32_t)kVec) : 0u;
+  const uint32_t block_end = min(block * s.block + s.block, s.n);
+  const uint32_t first = block * s.block + group * s.tile, last = min(first + s.tile, s.n);
+  if (count && first < last) {
+    bool head = first > 0 && s.key[first - 1] == s.key[first];
+    float8 sum = 0.0f;
+    for (uint32_t j = first; j < last; j += kTileStep) {
+      uint32_t key[kTileStep + 1], token[kTileStep];
 #pragma unroll
-    for (uint32_t u = 0; u < kTileStep; ++u) {
-      key[u] = s.key[j + u];
-      token[u] = s.token[j + u];
-    }
-    key[kTileStep] = j + kTileStep < s.n ? s.key[j + kTileStep] : ~0u;
-    if (key[0] >= vocab) break;
-    typename Packed<In>::type v[kTileStep];
-#pragma unroll
-    for (uint32_t u = 0; u < kTileStep; ++u)
-      if (j + u < last && key[u] < vocab)
-        v[u] = load_some((const In*)grad_out.data + row_offset(grad_out, token[u]) + col, count);
-#pragma unroll
-    for (uint32_t u = 0; u < kTileStep; ++u) {
-      if (j + u >= last || key[u] >= vocab) break;
-      sum += widen8<In>(v[u]);
-      const bool goes_on = j + u + 1 < s.n && key[u + 1] == key[u];
-      if (goes_on && j + u + 1 < last) continue;
-      if (head || goes_on) {
-        float* to = s.parts + ((uint64_t)tile * 2 + (head ? 0 : 1)) * s.stride + col;
-        store8(to, sum);
-      } else {
-        write_sum<Out>(grad, key[u], col, count, sum, scale, accumulate);
+      for (uint32_t u = 0; u < kTileStep; ++u) {
+        key[u] = s.key[j + u];
+        token[u] = s.token[j + u];
       }
-      head = false;
-      sum = 0.0f;
+      key[kTileStep] = j + kTileStep < s.n ? s.key[j + kTileStep] : ~0u;
+      if (key[0] >= vocab) break;
+      typename Packed<In>::type v[kTileStep];
+#pragma unroll
+      for (uint32_t u = 0; u < kTileStep; ++u)
+        if (j + u < last && key[u] < vocab)
+          v[u] = load_some((const In*)grad_out.data + row_offset(grad_out, token[u]) + col, count);
+#pragma unroll
+      for (uint32_t u = 0; u < kTileStep; ++u) {
+        if (j + u >= last || key[u] >= vocab) break;
+        sum += widen8<In>(v[u]);
+        const bool goes_on = j + u + 1 < s.n && key[u + 1] == key[u];
+        if (goes_on && j + u + 1 < last) continue;
+        if (head || goes_on) part[head ? 0 : 1][threadIdx.x] = sum;
+        else write_sum<Out>(grad, key[u], col, count, sum, scale, accumulate);
+        head = false;
+        sum = 0.0f;
+      }
     }
   }
+  __syncthreads();
+  if (group || !count) return;
+  // The first group goes through the tiles and puts together what crosses them; what crosses the
+  // block's ends is left to tile_join_kernel.
+  float* out = s.parts + (uint64_t)block * 2 * s.stride + col;
+  float8 sum = 0.0f;
+  bool open = false, began_before = false;
+  for (uint32_t g = 0, a = first; a < block_end; ++g, a += s.tile) {
+    const uint32_t b = min(a + s.tile, block_end), k0 = s.key[a], k1 = s.key[b - 1];
+    if (k0 >= vocab) break;
+    const uint32_t mine = (g << s.shift) + threadIdx.x;
+    const bool head = a > 0 && s.key[a - 1] == k0, goes_on = k1 < vocab && b < s.n && s.key[b] == k1;
+    if (head) {
+      if (g == 0) began_before = true;
+      sum += part[0][mine];
+      open = true;
+      if (k0 == k1 && goes_on) continue;   // the whole tile
+      if (began_before) store8(out, sum);
+      else write_sum<Out>(grad, k0, col, count, sum, scale, accumulate);
+      open = began_before = false;
+      sum = 0.0f;
+    }
+    if (goes_on) {
+      sum = part[1][mine];
+      open = true;
+    }
+  }
+  if (open) store8(out + (began_before ? 0 : s.stride), sum);
 }
 
-// Adds the parts of a sum that crosses tiles: a workgroup for every tile in which one begins and
+// Adds the parts of a sum that crosses blocks: a workgroup for every block in which one begins and
 // does not end, its four wavefronts a quarter of the parts each.
 template <typename Out>
 __global__ void __launch_bounds__(256)
 tile_join_kernel(TileView s, uint32_t width, float scale, bool accumulate, themis_rows_t grad, uint32_t vocab) {
   __shared__ float8 quarter[3][64];
-  const uint32_t tile = blockIdx.x, first = tile * s.tile, next = first + s.tile;
+  const uint32_t block = blockIdx.x, first = block * s.block, next = first + s.block;
   if (next >= s.n) return;
   const uint32_t v = s.key[next - 1];
   if (v >= vocab || s.key[next] != v) return;
   if (first > 0 && s.key[first - 1] == v) return;   // it began before
-  uint32_t lo = next, hi = s.n;   // where it ends
-  while (lo < hi) {
-    const uint32_t mid = lo + ((hi - lo) >> 1);
-    if (s.key[mid] <= v) lo = mid + 1;
-    else hi = mid;
-  }
-  const uint32_t more = (lo - 1) / s.tile - tile;   // parts behind the first
   const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
+  // The blocks behind this one that it reaches into: those whose first key is v.  Every lane looks
+  // at one of 64 places, which are nearer to each other each time.
+  uint32_t lo = block + 1, hi = s.blocks;   // block lo is one, block hi (if there is one) is none
+  while (hi - lo > 1) {
+    const uint32_t step = (hi - lo + 63) / 64;
+    const uint64_t at = (uint64_t)lo + (uint64_t)lane * step;
+    const uint64_t in = __ballot(at < hi && s.key[at * s.block] == v);   // (lane 0 is always in)
+    const uint32_t reach = 64 - (uint32_t)__builtin_clzll(in);           // the first place that is not
+    const uint32_t new_lo = lo + (reach - 1) * step;
+    hi = min(hi, new_lo + step);
+    lo = new_lo;
+  }
+  const uint32_t terms = lo - block + 1;
   const uint32_t col = (blockIdx.y * 64u + lane) * kVec;
   const bool on = col < width;
-  const uint32_t each = (more + 1 + 3) / 4, begin = min(wave * each, more + 1), end = min(begin + each, more + 1);
+  const uint32_t each = (terms + 3) / 4, begin = min(wave * each, terms), end = min(begin + each, terms);
   float8 sum = 0.0f;
   if (on) {
 #pragma unroll 8
     for (uint32_t p = begin; p < end; ++p)
-      sum += load8(s.parts + ((uint64_t)(tile + p) * 2 + (p == 0 ? 1 : 0)) * s.stride + col);
+      sum += load8(s.parts + ((uint64_t)(block + p) * 2 + (p == 0 ? 1 : 0)) * s.stride + col);
   }
   if (wave) quarter[wave - 1][lane] = sum;
   __syncthreads();

@@ -70,7 +70,7 @@ uint32_t next_power(uint32_t x) {   // the smallest p with 2^p >= x
 struct GradLayout {
   uint32_t passes, bits;           // of the sort
   uint32_t part, sort_parts;       // tokens of a workgroup, workgroups
-  uint32_t tile, tiles, slabs, shift, stride;
+  uint32_t tile, block, blocks, slabs, shift, stride;
   size_t key[2], token[2], counts, parts, bytes;
 };
 
@@ -80,16 +80,20 @@ GradLayout grad_layout(uint32_t n, uint32_t width, uint32_t vocab) {
   const uint32_t bits = next_power(vocab + 1);   // keys 0 .. vocab
   l.passes = (bits + 9) / 10;
   l.bits = (bits + l.passes - 1) / l.passes;
-  l.part = std::max(1024u, (uint32_t)(((uint64_t)n + 255) / 256 + kSortGroup - 1) / kSortGroup * kSortGroup);
+  // A workgroup of the sort takes kSortGroup tokens in one turn, and reads the counts of all parts,
+  // eight at a time: about as long, so there are ten parts for every turn.
+  l.part = kSortGroup;
+  while ((uint64_t)n > (uint64_t)l.part * (10 * (l.part / kSortGroup))) l.part *= 2;
   l.sort_parts = (n + l.part - 1) / l.part;
   const uint32_t vecs = (width + kVec - 1) / kVec;
-  l.shift = std::min(next_power(vecs), 6u);
+  l.shift = std::max(std::min(next_power(vecs), 6u), kLeastShift);
   l.slabs = (vecs + 63) / 64;
   l.stride = l.slabs * 512;
   // Tiles: long, so that few sums cross one, as long as there is a wavefront for every SIMD four times.
   l.tile = 128;
-  while (l.tile > 16 && (((uint64_t)n + l.tile - 1) / l.tile * l.slabs << l.shift) / 64 < 4096) l.tile /= 2;
-  l.tiles = (n + l.tile - 1) / l.tile;
+  while (l.tile > 8 && (((uint64_t)n + l.tile - 1) / l.tile * l.slabs << l.shift) / 64 < 4096) l.tile /= 2;
+  l.block = l.tile * (256u >> l.shift);
+  l.blocks = (n + l.block - 1) / l.block;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -102,7 +106,7 @@ GradLayout grad_layout(uint32_t n, uint32_t width, uint32_t vocab) {
     l.token[k] = take(list);
   }
   l.counts = take((size_t)l.sort_parts * (sizeof(uint32_t) << l.bits));
-  l.parts = take((size_t)l.tiles * 2 * l.stride * sizeof(float));
+  l.parts = take((size_t)l.blocks * 2 * l.stride * sizeof(float));
   l.bytes = at;
   return l;
 }
@@ -152,9 +156,8 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
   if (!rows_apart(*grad, vocab, width)) return THEMIS_ERR_INVALID_ARGUMENT;
   const GradLayout l = grad_layout((uint32_t)n, (uint32_t)width, (uint32_t)vocab);
   if (l.bytes && (!workspace || workspace_bytes < l.bytes || !aligned(workspace, 16))) return THEMIS_ERR_WORKSPACE;
-  const uint64_t items = (uint64_t)l.tiles * l.slabs, per_group = 256u >> l.shift;
-  const uint64_t tile_groups = (items + per_group - 1) / per_group;
-  if (tile_groups > 1u << 23 || l.slabs > 65535) return THEMIS_ERR_UNSUPPORTED;   // (grids of less than 2^32 lanes)
+  const uint64_t sums = (uint64_t)l.blocks * l.slabs;
+  if (sums > 1u << 23 || l.slabs > 65535) return THEMIS_ERR_UNSUPPORTED;   // (grids of less than 2^32 lanes)
   const themis_rows_t none = {nullptr, THEMIS_F32, 1, 0, 0};
   const themis_rows_t g = n ? *grad_out : none, k = n ? *ids : none;
   const uint32_t skip = ignored >= 0 && (uint64_t)ignored < vocab ? (uint32_t)ignored : ~0u;
@@ -182,24 +185,24 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
   t.token = token[(l.passes - 1) & 1];
   t.n = (uint32_t)n;
   t.tile = l.tile;
-  t.tiles = l.tiles;
+  t.block = l.block;
+  t.blocks = l.blocks;
   t.slabs = l.slabs;
   t.shift = l.shift;
   t.parts = (float*)(at + l.parts);
   t.stride = l.stride;
-  t.tile_groups = (uint32_t)tile_groups;
   // (a workgroup's zeros: about 256 KiB, in up to 64 rows)
   t.fill_rows = (uint32_t)std::min<uint64_t>(64, std::max<uint64_t>(1, (256u << 10) / (width * type_bytes(grad->type))));
   const uint64_t fill = accumulate ? 0 : std::min<uint64_t>((vocab + t.fill_rows - 1) / t.fill_rows, 1u << 20);
   with_type(g.type, [&](auto in) {
     with_type(grad->type, [&](auto to) {
-      go(tile_sum_kernel<decltype(in), decltype(to)>, dim3(t.tile_groups + (uint32_t)fill), 256, t, g, (uint32_t)width,
+      go(tile_sum_kernel<decltype(in), decltype(to)>, dim3((uint32_t)(sums + fill)), 256, t, g, (uint32_t)width,
          scale, accumulate != 0, *grad, (uint32_t)vocab);
     });
   });
-  if (l.tiles > 1)
+  if (l.blocks > 1)
     with_type(grad->type, [&](auto to) {
-      go(tile_join_kernel<decltype(to)>, dim3(l.tiles - 1, l.slabs), 256, t, (uint32_t)width, scale, accumulate != 0,
+      go(tile_join_kernel<decltype(to)>, dim3(l.blocks - 1, l.slabs), 256, t, (uint32_t)width, scale, accumulate != 0,
          *grad, (uint32_t)vocab);
     });
   return go.status();
