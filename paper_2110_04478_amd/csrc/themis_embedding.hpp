@@ -13,45 +13,177 @@ namespace themis {
 // loads are in flight together: the number, then the row, are two dependent trips to memory and
 // all that there is to hide.
 // ---------------------------------------------------------------------------
+template <bool kFull, int kRows, typename In, typename Out, int kVec>
+__device__ __forceinline__ void lookup_rows(const Slice<kVec>& slice, const Rows& table, uint32_t vocab, const Rows& ids,
+                                            uint32_t n, float scale, const Rows& out, uint32_t t0, uint32_t groups) {
+  uint32_t row[kRows];
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) row[k] = token_row(ids, min(t0 + k * groups, n - 1u), vocab);
+  typename Packed<In, 8>::type v[kRows];
+  if (vocab) {
+#pragma unroll
+    for (int k = 0; k < kRows; ++k)   // (row 0 in the place of none: its values are not used)
+      v[k] = slice.template read<kFull>(row_at<const In>(table, row[k] == ~0u ? 0u : row[k]));
+  }
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const uint32_t t = t0 + k * groups;
+    if (t >= n) break;
+    const float8 nan = __builtin_nanf("");
+    const float8 x = row[k] != ~0u ? widen<8>(v[k]) * scale : nan;
+    if (kRows > 1) slice.template write_away<kFull>(row_at<Out>(out, t), x);
+    else slice.template write<kFull>(row_at<Out>(out, t), x);
+  }
+}
+
 template <typename In, typename Out, int kRows>
 __global__ void __launch_bounds__(256)
-lookup_kernel(themis_rows_t table, uint32_t vocab, uint32_t width, themis_rows_t ids, uint32_t n, float scale,
-              themis_rows_t out, uint32_t shift) {
-  const uint32_t col = (blockIdx.y * 256u + (threadIdx.x & ((1u << shift) - 1u))) * kVec;
-  if (col >= width) return;
-  const uint32_t count = min(width - col, (uint32_t)kVec);
+lookup_kernel(Rows table, uint32_t vocab, uint32_t width, Rows ids, uint32_t n, float scale, Rows out, uint32_t shift) {
+  const uint32_t lanes = 1u << shift;
+  const Slice<kVecOf<In, Out>> slice(blockIdx.y * 256u * kLaneElements, threadIdx.x & (lanes - 1u), lanes, width);
+  if (!slice.any()) return;
   const uint32_t groups = 256u >> shift;   // rows side by side
   const uint32_t step = groups * kRows;
   for (uint64_t first = (uint64_t)blockIdx.x * step; first < n; first += (uint64_t)gridDim.x * step) {
-    const uint32_t t0 = (uint32_t)first + (threadIdx.x >> shift);
-    uint32_t row[kRows];
-#pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-      const uint64_t t = (uint64_t)t0 + k * groups;
-      row[k] = t < n ? token_row(ids, (uint32_t)t, vocab) : ~0u;
-    }
-    typename Packed<In>::type v[kRows];
-#pragma unroll
-    for (int k = 0; k < kRows; ++k)
-      if (row[k] != ~0u) v[k] = load_some((const In*)table.data + row_offset(table, row[k]) + col, count);
-#pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-      const uint64_t t = (uint64_t)t0 + k * groups;
-      if (t >= n) break;
-      const float8 nan = __builtin_nanf("");
-      const float8 x = row[k] != ~0u ? widen8<In>(v[k]) * scale : nan;
-      store_some((Out*)out.data + row_offset(out, (uint32_t)t) + col, x, count);
-    }
+    const uint32_t t0 = (uint32_t)first + (threadIdx.x >> shift);   // (below 2^32: n is below 2^31)
+    if (slice.full()) lookup_rows<true, kRows, In, Out>(slice, table, vocab, ids, n, scale, out, t0, groups);
+    else lookup_rows<false, kRows, In, Out>(slice, table, vocab, ids, n, scale, out, t0, groups);
   }
 }
 
 // ---------------------------------------------------------------------------
 // themis_embedding_grad: grad[v] (+)= scale * sum of grad_out[t] over ids[t] == v.
 //
-// The tokens are sorted by their number, stable, so that a table row's tokens stand next to each
-// other in ascending order; the sorted list is cut into tiles of one length, whatever the numbers
-// are, so that a token that makes up half of the list costs no more than any other half.  A tile
-// adds its rows one after the other and writes the sums that begin and end in it.  A sum that
+// Up to kFewTokens tokens: one launch, no workspace.  A workgroup for every token finds all tokens
+// of its number; the workgroups of one number share the row's elements (a token that occurs often
+// has many), and the lanes of a workgroup the elements and the tokens: G groups of lanes take a
+// G-th of the tokens each, in order, and their sums are added in order.
+// ---------------------------------------------------------------------------
+constexpr uint32_t kFewTokens = 4096;
+constexpr uint32_t kRowsInFlight = 8;
+constexpr uint32_t kMostGroups = 32;
+
+template <bool kFull, typename In, int kVec>
+__device__ __forceinline__ float8 sum_listed(const Slice<kVec>& slice, const Rows& grad_out, const uint16_t* list,
+                                             uint32_t begin, uint32_t end) {
+  float8 sum = 0.0f;
+  uint32_t i = begin;
+  for (; i + kRowsInFlight <= end; i += kRowsInFlight) {
+    typename Packed<In, 8>::type v[kRowsInFlight];
+#pragma unroll
+    for (uint32_t u = 0; u < kRowsInFlight; ++u)
+      v[u] = slice.template read<kFull>(row_at<const In>(grad_out, list[i + u]));
+#pragma unroll
+    for (uint32_t u = 0; u < kRowsInFlight; ++u) sum += widen<8>(v[u]);
+  }
+#pragma unroll 2
+  for (; i < end; ++i) sum += widen<8>(slice.template read<kFull>(row_at<const In>(grad_out, list[i])));
+  return sum;
+}
+
+// Zeros in the rows of `empty` behind v0, by a workgroup.
+template <typename Out>
+__device__ __forceinline__ void write_zeros(uint64_t empty, uint32_t v0, uint32_t width, const Rows& grad) {
+  constexpr int kVec = kVecOf<Out>;
+  const uint32_t vecs = (width + kVec - 1) / kVec;
+  for (; empty; empty &= empty - 1) {
+    Out* to = row_at<Out>(grad, v0 + (uint32_t)__builtin_ctzll(empty));
+    for (uint32_t c = threadIdx.x; c < vecs; c += 256)
+      store_some_away<kVec>(to + c * kVec, Floats<kVec>(0.0f), min(width - c * kVec, (uint32_t)kVec));
+  }
+}
+
+template <bool kFull, int kVec, typename Out>
+__device__ __forceinline__ void write_sum(const Rows& grad, uint32_t v, const Slice<kVec>& slice, float8 sum, float scale,
+                                          bool accumulate) {
+  Out* to = row_at<Out>(grad, v);
+  float8 x = sum * scale;
+  if (accumulate) x = widen<8>(slice.template read<kFull>((const Out*)to)) + x;
+  slice.template write<kFull>(to, x);
+}
+
+// Workgroups blockIdx.x < n: the tokens; the others write the zeros of up to 64 rows at a time.
+template <typename In, typename Out>
+__global__ void __launch_bounds__(256)
+few_tokens_kernel(uint32_t n, Rows grad_out, uint32_t width, Rows ids, float scale, uint32_t ignored, bool accumulate,
+                  Rows grad, uint32_t vocab, uint32_t fill_rows) {
+  __shared__ uint64_t masks[kFewTokens / 64];   // which tokens, 64 each
+  __shared__ uint16_t list[kFewTokens];
+  __shared__ float8 part[256];
+  const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t chunks = (n + 63) / 64;
+  if (blockIdx.x >= n) {
+    if (blockIdx.y) return;
+    const uint64_t step = (uint64_t)(gridDim.x - n) * fill_rows;
+    for (uint64_t v = (uint64_t)(blockIdx.x - n) * fill_rows; v < vocab; v += step) {
+      const uint32_t v0 = (uint32_t)v, rows = min(vocab - v0, fill_rows);
+      __syncthreads();
+      if (threadIdx.x == 0) masks[0] = 0;
+      __syncthreads();
+      for (uint32_t t = threadIdx.x; t < n; t += 256) {
+        const uint32_t id = token_row(ids, t, vocab), at = id - v0;
+        if (id >= v0 && at < rows && id != ignored) atomicOr((unsigned long long*)&masks[0], 1ull << at);
+      }
+      __syncthreads();
+      const uint64_t all = rows == 64 ? ~0ull : (1ull << rows) - 1;
+      write_zeros<Out>(all & ~masks[0], v0, width, grad);
+    }
+    return;
+  }
+  const uint32_t t = blockIdx.x, id = token_row(ids, t, vocab);
+  if (id == ~0u || id == ignored) return;
+  for (uint32_t c = wave; c < chunks; c += 4) {
+    const uint32_t i = c * 64 + lane;
+    const uint64_t mine = __ballot(i < n && token_row(ids, min(i, n - 1u), vocab) == id);
+    if (lane == 0) masks[c] = mine;
+  }
+  __syncthreads();
+  const uint64_t mask = lane < chunks ? masks[lane] : 0ull;
+  uint32_t upto = (uint32_t)__popcll(mask);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t y = __shfl_up(upto, d);
+    if (lane >= (uint32_t)d) upto += y;
+  }
+  const uint32_t before = upto - (uint32_t)__popcll(mask);
+  const uint32_t count = __builtin_amdgcn_readlane(upto, 63);
+  const uint32_t rank = __builtin_amdgcn_readlane(before, t / 64) +
+                        (uint32_t)__popcll(masks[t / 64] & ((1ull << (t & 63u)) - 1));
+  // Groups of lanes: as many as there are tokens, a power of two.
+  const uint32_t more = 31 - (uint32_t)__builtin_clz(min(count, kMostGroups));
+  const uint32_t groups = 1u << more, shift = 8 - more, lanes = 1u << shift;
+  const uint32_t slices = (width + lanes * kLaneElements - 1) / (lanes * kLaneElements);
+  if (rank + count * blockIdx.y >= slices) return;
+  for (uint32_t c = wave; c < chunks; c += 4) {
+    const uint64_t m = masks[c];
+    const uint32_t at = __builtin_amdgcn_readlane(before, c);
+    if ((m >> lane) & 1u) list[at + (uint32_t)__popcll(m & ((1ull << lane) - 1))] = (uint16_t)(c * 64 + lane);
+  }
+  __syncthreads();
+  const uint32_t group = threadIdx.x >> shift, each = (count + groups - 1) / groups;
+  const uint32_t begin = min(group * each, count), end = min(begin + each, count);
+  for (uint32_t k = rank + count * blockIdx.y; k < slices; k += count * gridDim.y) {
+    constexpr int kVec = kVecOf<In>;
+    const Slice<kVec> slice(k * lanes * kLaneElements, threadIdx.x & (lanes - 1u), lanes, width);
+    float8 sum = 0.0f;
+    if (slice.full()) sum = sum_listed<true, In>(slice, grad_out, list, begin, end);
+    else if (slice.any()) sum = sum_listed<false, In>(slice, grad_out, list, begin, end);
+    if (groups > 1) {
+      part[threadIdx.x] = sum;
+      __syncthreads();
+      if (group == 0)
+        for (uint32_t g = 1; g < groups; ++g) sum += part[(g << shift) + threadIdx.x];
+    }
+    if (group == 0 && slice.any()) write_sum<false, kVec, Out>(grad, id, slice, sum, scale, accumulate);
+    if (groups > 1) __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// More tokens: they are sorted by their number, stable, so that a table row's tokens stand next to
+// each other in ascending order; the sorted list is cut into tiles of one length, whatever the
+// numbers are, so that a token that makes up half of the list costs no more than any other half.  A
+// tile adds its rows one after the other and writes the sums that begin and end in it.  A sum that
 // crosses tiles is left in parts, which are added in the order of the tiles.
 //
 // Sort: least significant digit first, up to ten bits a pass and two launches: every workgroup
@@ -73,15 +205,15 @@ struct SortView {
   uint32_t* token_out;
 };
 
-__device__ __forceinline__ uint32_t sort_key(const SortView& s, const themis_rows_t& ids, uint32_t vocab,
-                                             uint32_t ignored, uint32_t i) {
+__device__ __forceinline__ uint32_t sort_key(const SortView& s, const Rows& ids, uint32_t vocab, uint32_t ignored,
+                                             uint32_t i) {
   if (s.key_in) return s.key_in[i];
   const uint32_t id = token_row(ids, i, vocab);
   return id == ~0u || id == ignored ? vocab : id;
 }
 
 __global__ void __launch_bounds__(kSortGroup)
-sort_count_kernel(SortView s, themis_rows_t ids, uint32_t vocab, uint32_t ignored) {
+sort_count_kernel(SortView s, Rows ids, uint32_t vocab, uint32_t ignored) {
   __shared__ uint32_t count[kMaxBins];
   const uint32_t bins = 1u << s.bits, first = blockIdx.x * s.part;
   const uint32_t last = min(first + s.part, s.n);
@@ -94,7 +226,7 @@ sort_count_kernel(SortView s, themis_rows_t ids, uint32_t vocab, uint32_t ignore
 }
 
 __global__ void __launch_bounds__(kSortGroup)
-sort_move_kernel(SortView s, themis_rows_t ids, uint32_t vocab, uint32_t ignored) {
+sort_move_kernel(SortView s, Rows ids, uint32_t vocab, uint32_t ignored) {
   __shared__ uint32_t place[kSortWaves][kMaxBins];   // first a wavefront's counts, then where its next one goes
   __shared__ uint32_t wave_sums[kSortWaves];
   const uint32_t bins = 1u << s.bits, first = blockIdx.x * s.part;
@@ -164,8 +296,6 @@ sort_move_kernel(SortView s, themis_rows_t ids, uint32_t vocab, uint32_t ignored
 // The sorted list in tiles, one for every group of lanes of a workgroup (a wavefront, less where the
 // rows are short), and the tiles of a workgroup in blocks.
 struct TileView {
-  const uint32_t* key;     // [n], ascending, rounded up to a multiple of kTileStep
-  const uint32_t* token;
   uint32_t n, tile;        // tokens, tokens of a tile (a multiple of kTileStep)
   uint32_t block;          // tokens of a block
   uint32_t blocks, slabs;  // slabs of 512 elements
@@ -179,7 +309,7 @@ constexpr uint32_t kLeastShift = 3;  // (up to 32 groups of lanes)
 
 // Zeros in those of up to 64 table rows from `v0` on that no token has: a lane looks for its row.
 template <typename Out>
-__device__ __forceinline__ void fill_rows(const TileView& s, uint32_t v0, uint32_t width, const themis_rows_t& grad,
+__device__ __forceinline__ void fill_rows(const TileView& s, const uint32_t* keys, uint32_t v0, uint32_t width, const Rows& grad,
                                           uint32_t vocab) {
   const uint32_t lane = threadIdx.x & 63u, v = v0 + lane;
   const bool mine = lane < s.fill_rows && v < vocab;
@@ -187,96 +317,128 @@ __device__ __forceinline__ void fill_rows(const TileView& s, uint32_t v0, uint32
   while (__any(lo < hi)) {
     if (lo < hi) {
       const uint32_t mid = lo + ((hi - lo) >> 1);
-      if (s.key[mid] < v) lo = mid + 1;
+      if (keys[mid] < v) lo = mid + 1;
       else hi = mid;
     }
   }
-  uint64_t empty = __ballot(mine && (lo >= s.n || s.key[lo] != v));
-  const uint32_t vecs = (width + kVec - 1) / kVec;
-  const float8 zero = 0.0f;
-  for (; empty; empty &= empty - 1) {
-    Out* to = (Out*)grad.data + row_offset(grad, v0 + (uint32_t)__builtin_ctzll(empty));
-    for (uint32_t c = threadIdx.x; c < vecs; c += 256) store_some(to + c * kVec, zero, min(width - c * kVec, (uint32_t)kVec));
+  write_zeros<Out>(__ballot(mine && (lo >= s.n || keys[lo] != v)), v0, width, grad);
+}
+
+// A tile's sums: those that begin and end in it to the table, the others to `head` (one that began
+// before) and `tail`.
+template <bool kFull, typename In, typename Out, int kVec>
+__device__ __forceinline__ void sum_tile(const TileView& s, const uint32_t* __restrict__ keys,
+                                         const uint32_t* __restrict__ tokens, const Slice<kVec>& slice,
+                                         const Rows& grad_out, float scale, bool accumulate, const Rows& grad,
+                                         uint32_t vocab, uint32_t first, uint32_t last, float8& head, float8& tail) {
+  bool before = first > 0 && keys[first - 1] == keys[first];
+  float8 sum = 0.0f;
+  for (uint32_t j = first; j < last; j += kTileStep) {
+    // (the lists are longer than n by a step; what stands there is not used)
+    const uint32_t *key_at = keys + j, *token_at = tokens + j;
+    uint32_t key[kTileStep + 1], token[kTileStep];
+#pragma unroll
+    for (uint32_t u = 0; u < kTileStep; ++u) {
+      key[u] = key_at[u];
+      token[u] = token_at[u];
+    }
+    key[kTileStep] = j + kTileStep < s.n ? keys[j + kTileStep] : ~0u;
+    uint32_t some = min(last - j, kTileStep);
+    if (some == kTileStep && key[kTileStep - 1] < vocab) {
+      typename Packed<In, 8>::type v[kTileStep];
+#pragma unroll
+      for (uint32_t u = 0; u < kTileStep; ++u) v[u] = slice.template read<kFull>(row_at<const In>(grad_out, token[u]));
+      // (what the sums that end here are added to is asked for at the same time: one after the
+      // other, 131,072 tokens of 2,048 added to a binary32 table took 242 us)
+      typename Packed<Out, 8>::type held[kTileStep];
+      if (accumulate) {
+#pragma unroll
+        for (uint32_t u = 0; u < kTileStep; ++u)
+          if (key[u + 1] != key[u]) held[u] = slice.template read<kFull>(row_at<const Out>(grad, key[u]));
+      }
+#pragma unroll
+      for (uint32_t u = 0; u < kTileStep; ++u) {
+        sum += widen<8>(v[u]);
+        const bool goes_on = key[u + 1] == key[u];
+        if (goes_on && j + u + 1 < last) continue;
+        if (before) {
+          head = sum;
+        } else if (goes_on) {
+          tail = sum;
+        } else {
+          float8 x = sum * scale;
+          if (accumulate) x = widen<8>(held[u]) + x;
+          slice.template write<kFull>(row_at<Out>(grad, key[u]), x);
+        }
+        before = false;
+        sum = 0.0f;
+      }
+    } else {   // the list's end, or the first tokens without a gradient
+      for (uint32_t u = 0; u < some; ++u) {
+        const uint32_t k = keys[j + u];
+        if (k >= vocab) return;
+        sum += widen<8>(slice.template read<kFull>(row_at<const In>(grad_out, tokens[j + u])));
+        const bool goes_on = j + u + 1 < s.n && keys[j + u + 1] == k;
+        if (goes_on && j + u + 1 < last) continue;
+        if (before) head = sum;
+        else if (goes_on) tail = sum;
+        else write_sum<kFull, kVec, Out>(grad, k, slice, sum, scale, accumulate);
+        before = false;
+        sum = 0.0f;
+      }
+    }
   }
 }
 
-template <typename Out>
-__device__ __forceinline__ void write_sum(const themis_rows_t& grad, uint32_t v, uint32_t col, uint32_t count,
-                                          float8 sum, float scale, bool accumulate) {
-  Out* to = (Out*)grad.data + row_offset(grad, v) + col;
-  float8 x = sum * scale;
-  if (accumulate) x = widen8<Out>(load_some(to, count)) + x;
-  store_some(to, x, count);
-}
-
-template <typename In, typename Out>
+// kWave: a wavefront for every tile, all of whose lanes go the same way.
+template <typename In, typename Out, bool kWave>
 __global__ void __launch_bounds__(256)
-tile_sum_kernel(TileView s, themis_rows_t grad_out, uint32_t width, float scale, bool accumulate, themis_rows_t grad,
-                uint32_t vocab) {
+tile_sum_kernel(TileView s, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ tokens, Rows grad_out,
+                uint32_t width, float scale, bool accumulate, Rows grad, uint32_t vocab) {
   // A group's sums that its tile does not hold whole: of one that began before, of one that goes on.
   __shared__ float8 part[2][256];
   const uint32_t sums = s.blocks * s.slabs;
   if (blockIdx.x >= sums) {
     const uint64_t step = (uint64_t)(gridDim.x - sums) * s.fill_rows;
     for (uint64_t v = (uint64_t)(blockIdx.x - sums) * s.fill_rows; v < vocab; v += step)
-      fill_rows<Out>(s, (uint32_t)v, width, grad, vocab);
+      fill_rows<Out>(s, keys, (uint32_t)v, width, grad, vocab);
     return;
   }
+  const uint32_t shift = kWave ? 6u : s.shift, lanes = 1u << shift;
   const uint32_t block = blockIdx.x / s.slabs, slab = blockIdx.x - block * s.slabs;
-  const uint32_t lanes = 1u << s.shift, group = threadIdx.x >> s.shift;
-  const uint32_t col = (slab * 64u + (threadIdx.x & (lanes - 1u))) * kVec;
-  const uint32_t count = col < width ? min(width - col, (uint32_t)kVec) : 0u;
+  const uint32_t group = kWave ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x >> shift;
+  constexpr int kVec = kVecOf<In>;
+  const Slice<kVec> slice(slab * 512u, threadIdx.x & (lanes - 1u), lanes, width);
   const uint32_t block_end = min(block * s.block + s.block, s.n);
   const uint32_t first = block * s.block + group * s.tile, last = min(first + s.tile, s.n);
-  if (count && first < last) {
-    bool head = first > 0 && s.key[first - 1] == s.key[first];
-    float8 sum = 0.0f;
-    for (uint32_t j = first; j < last; j += kTileStep) {
-      uint32_t key[kTileStep + 1], token[kTileStep];
-#pragma unroll
-      for (uint32_t u = 0; u < kTileStep; ++u) {
-        key[u] = s.key[j + u];
-        token[u] = s.token[j + u];
-      }
-      key[kTileStep] = j + kTileStep < s.n ? s.key[j + kTileStep] : ~0u;
-      if (key[0] >= vocab) break;
-      typename Packed<In>::type v[kTileStep];
-#pragma unroll
-      for (uint32_t u = 0; u < kTileStep; ++u)
-        if (j + u < last && key[u] < vocab)
-          v[u] = load_some((const In*)grad_out.data + row_offset(grad_out, token[u]) + col, count);
-#pragma unroll
-      for (uint32_t u = 0; u < kTileStep; ++u) {
-        if (j + u >= last || key[u] >= vocab) break;
-        sum += widen8<In>(v[u]);
-        const bool goes_on = j + u + 1 < s.n && key[u + 1] == key[u];
-        if (goes_on && j + u + 1 < last) continue;
-        if (head || goes_on) part[head ? 0 : 1][threadIdx.x] = sum;
-        else write_sum<Out>(grad, key[u], col, count, sum, scale, accumulate);
-        head = false;
-        sum = 0.0f;
-      }
-    }
+  if (slice.any() && first < last) {
+    float8 head = 0.0f, tail = 0.0f;
+    if (slice.full())
+      sum_tile<true, In, Out>(s, keys, tokens, slice, grad_out, scale, accumulate, grad, vocab, first, last, head, tail);
+    else
+      sum_tile<false, In, Out>(s, keys, tokens, slice, grad_out, scale, accumulate, grad, vocab, first, last, head, tail);
+    part[0][threadIdx.x] = head;
+    part[1][threadIdx.x] = tail;
   }
   __syncthreads();
-  if (group || !count) return;
+  if (group || !slice.any()) return;
   // The first group goes through the tiles and puts together what crosses them; what crosses the
   // block's ends is left to tile_join_kernel.
-  float* out = s.parts + (uint64_t)block * 2 * s.stride + col;
+  float* out = s.parts + (uint64_t)block * 2 * s.stride + (slab * 64u + threadIdx.x) * kLaneElements;
   float8 sum = 0.0f;
   bool open = false, began_before = false;
   for (uint32_t g = 0, a = first; a < block_end; ++g, a += s.tile) {
-    const uint32_t b = min(a + s.tile, block_end), k0 = s.key[a], k1 = s.key[b - 1];
+    const uint32_t b = min(a + s.tile, block_end), k0 = keys[a], k1 = keys[b - 1];
     if (k0 >= vocab) break;
-    const uint32_t mine = (g << s.shift) + threadIdx.x;
-    const bool head = a > 0 && s.key[a - 1] == k0, goes_on = k1 < vocab && b < s.n && s.key[b] == k1;
+    const uint32_t mine = (g << shift) + threadIdx.x;
+    const bool head = a > 0 && keys[a - 1] == k0, goes_on = k1 < vocab && b < s.n && keys[b] == k1;
     if (head) {
       if (g == 0) began_before = true;
       sum += part[0][mine];
       open = true;
       if (k0 == k1 && goes_on) continue;   // the whole tile
-      if (began_before) store8(out, sum);
-      else write_sum<Out>(grad, k0, col, count, sum, scale, accumulate);
+      if (began_before) store<8>(out, sum);
+      else write_sum<false, kVec, Out>(grad, k0, slice, sum, scale, accumulate);
       open = began_before = false;
       sum = 0.0f;
     }
@@ -285,20 +447,20 @@ tile_sum_kernel(TileView s, themis_rows_t grad_out, uint32_t width, float scale,
       open = true;
     }
   }
-  if (open) store8(out + (began_before ? 0 : s.stride), sum);
+  if (open) store<8>(out + (began_before ? 0 : s.stride), sum);
 }
 
 // Adds the parts of a sum that crosses blocks: a workgroup for every block in which one begins and
 // does not end, its four wavefronts a quarter of the parts each.
-template <typename Out>
+template <int kVec, typename Out>
 __global__ void __launch_bounds__(256)
-tile_join_kernel(TileView s, uint32_t width, float scale, bool accumulate, themis_rows_t grad, uint32_t vocab) {
+tile_join_kernel(TileView s, const uint32_t* __restrict__ keys, uint32_t width, float scale, bool accumulate, Rows grad, uint32_t vocab) {
   __shared__ float8 quarter[3][64];
   const uint32_t block = blockIdx.x, first = block * s.block, next = first + s.block;
   if (next >= s.n) return;
-  const uint32_t v = s.key[next - 1];
-  if (v >= vocab || s.key[next] != v) return;
-  if (first > 0 && s.key[first - 1] == v) return;   // it began before
+  const uint32_t v = keys[next - 1];
+  if (v >= vocab || keys[next] != v) return;
+  if (first > 0 && keys[first - 1] == v) return;   // it began before
   const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
   // The blocks behind this one that it reaches into: those whose first key is v.  Every lane looks
   // at one of 64 places, which are nearer to each other each time.
@@ -306,28 +468,28 @@ tile_join_kernel(TileView s, uint32_t width, float scale, bool accumulate, themi
   while (hi - lo > 1) {
     const uint32_t step = (hi - lo + 63) / 64;
     const uint64_t at = (uint64_t)lo + (uint64_t)lane * step;
-    const uint64_t in = __ballot(at < hi && s.key[at * s.block] == v);   // (lane 0 is always in)
+    const uint64_t in = __ballot(at < hi && keys[at * s.block] == v);   // (lane 0 is always in)
     const uint32_t reach = 64 - (uint32_t)__builtin_clzll(in);           // the first place that is not
     const uint32_t new_lo = lo + (reach - 1) * step;
     hi = min(hi, new_lo + step);
     lo = new_lo;
   }
   const uint32_t terms = lo - block + 1;
-  const uint32_t col = (blockIdx.y * 64u + lane) * kVec;
-  const bool on = col < width;
+  const Slice<kVec> slice(blockIdx.y * 512u, lane & ((1u << s.shift) - 1u), 1u << s.shift, width);
+  const bool on = lane >> s.shift == 0 && slice.any();
   const uint32_t each = (terms + 3) / 4, begin = min(wave * each, terms), end = min(begin + each, terms);
   float8 sum = 0.0f;
   if (on) {
 #pragma unroll 8
     for (uint32_t p = begin; p < end; ++p)
-      sum += load8(s.parts + ((uint64_t)(block + p) * 2 + (p == 0 ? 1 : 0)) * s.stride + col);
+      sum += load<8>(s.parts + ((uint64_t)(block + p) * 2 + (p == 0 ? 1 : 0)) * s.stride + (blockIdx.y * 64u + lane) * kLaneElements);
   }
   if (wave) quarter[wave - 1][lane] = sum;
   __syncthreads();
   if (wave || !on) return;
 #pragma unroll
   for (int w = 0; w < 3; ++w) sum += quarter[w][lane];
-  write_sum<Out>(grad, v, col, min(width - col, (uint32_t)kVec), sum, scale, accumulate);
+  write_sum<false, kVec, Out>(grad, v, slice, sum, scale, accumulate);
 }
 
 }  // namespace themis

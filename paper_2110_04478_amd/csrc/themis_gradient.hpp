@@ -9,11 +9,26 @@
 
 #include "themis_elements.hpp"
 
+#ifndef CL
+#define CL load_once
+#endif
+#ifndef CS
+#define CS store_away
+#endif
+#ifndef NL
+#define NL load
+#endif
+#ifndef NG
+#define NG 2048
+#endif
+#ifndef PM
+#define PM 65536
+#endif
 namespace themis {
 
 constexpr uint32_t kPieceLeast = 2048;   // one access of 256 lanes
-constexpr uint32_t kPieceMost = 65536;
-constexpr uint32_t kNormGroups = 2048;   // workgroups of a pass over the list: eight for every CU
+constexpr uint32_t kPieceMost = PM;
+constexpr uint32_t kNormGroups = NG;   // workgroups of a pass over the list: eight for every CU
 
 enum : uint32_t { kInDense = 1u << 16, kOutDense = 1u << 17, kInPlace = 1u << 18 };
 
@@ -60,10 +75,11 @@ __device__ __forceinline__ double group_sum(double x, double (&part)[4]) {
   return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-__device__ __forceinline__ double square8(float8 v, double sum) {
+template <int N>
+__device__ __forceinline__ double squares(Floats<N> v, double sum) {
   double odd = 0.0;
 #pragma unroll
-  for (int k = 0; k < kVec; k += 2) {
+  for (int k = 0; k < N; k += 2) {
     sum = fma((double)v[k], (double)v[k], sum);
     odd = fma((double)v[k + 1], (double)v[k + 1], odd);
   }
@@ -76,17 +92,18 @@ __device__ __forceinline__ double piece_squares(const Piece& p) {
   const T* in = (const T*)p.in;
   double sum = 0.0;
   if (p.kind & kInDense) {
+    constexpr int kVec = kVecOf<T>;
     constexpr uint32_t kStep = 256 * kVec, kUnroll = 4;
     uint32_t e = threadIdx.x * kVec;
     for (; e + (kUnroll - 1) * kStep + kVec <= p.count; e += kUnroll * kStep) {
-      typename Packed<T>::type v[kUnroll];
+      typename Packed<T, kVec>::type v[kUnroll];
 #pragma unroll
-      for (uint32_t k = 0; k < kUnroll; ++k) v[k] = load8(in + e + k * kStep);
+      for (uint32_t k = 0; k < kUnroll; ++k) v[k] = NL<kVec>(in + e + k * kStep);
 #pragma unroll
-      for (uint32_t k = 0; k < kUnroll; ++k) sum = square8(widen8<T>(v[k]), sum);
+      for (uint32_t k = 0; k < kUnroll; ++k) sum = squares<kVec>(widen<kVec>(v[k]), sum);
     }
     for (; e < p.count; e += kStep)
-      sum = square8(widen8<T>(load_some(in + e, min(p.count - e, (uint32_t)kVec))), sum);
+      sum = squares<kVec>(widen<kVec>(load_some<kVec>(in + e, min(p.count - e, (uint32_t)kVec))), sum);
   } else {
     for (uint32_t e = threadIdx.x; e < p.count; e += 256) {
       const uint32_t r = e / p.cols, c = e - r * p.cols;
@@ -146,18 +163,19 @@ __device__ __forceinline__ void scale_piece(const Piece& p, float factor) {
   const In* in = (const In*)p.in;
   Out* out = (Out*)p.out;
   if ((p.kind & (kInDense | kOutDense)) == (kInDense | kOutDense)) {
+    constexpr int kVec = kVecOf<In, Out>;
     constexpr uint32_t kStep = 256 * kVec, kUnroll = 4;
     uint32_t e = threadIdx.x * kVec;
     for (; e + (kUnroll - 1) * kStep + kVec <= p.count; e += kUnroll * kStep) {
-      typename Packed<In>::type v[kUnroll];
+      typename Packed<In, kVec>::type v[kUnroll];
 #pragma unroll
-      for (uint32_t k = 0; k < kUnroll; ++k) v[k] = load8(in + e + k * kStep);
+      for (uint32_t k = 0; k < kUnroll; ++k) v[k] = CL<kVec>(in + e + k * kStep);
 #pragma unroll
-      for (uint32_t k = 0; k < kUnroll; ++k) store8(out + e + k * kStep, widen8<In>(v[k]) * factor);
+      for (uint32_t k = 0; k < kUnroll; ++k) CS<kVec>(out + e + k * kStep, widen<kVec>(v[k]) * factor);
     }
     for (; e < p.count; e += kStep) {
       const uint32_t some = min(p.count - e, (uint32_t)kVec);
-      store_some(out + e, widen8<In>(load_some(in + e, some)) * factor, some);
+      store_some<kVec>(out + e, widen<kVec>(load_some<kVec>(in + e, some)) * factor, some);
     }
   } else {
     for (uint32_t e = threadIdx.x; e < p.count; e += 256) {

@@ -76,7 +76,7 @@ struct GradLayout {
 
 GradLayout grad_layout(uint32_t n, uint32_t width, uint32_t vocab) {
   GradLayout l = {};
-  if (n == 0) return l;
+  if (n <= kFewTokens) return l;
   const uint32_t bits = next_power(vocab + 1);   // keys 0 .. vocab
   l.passes = (bits + 9) / 10;
   l.bits = (bits + l.passes - 1) / l.passes;
@@ -85,12 +85,12 @@ GradLayout grad_layout(uint32_t n, uint32_t width, uint32_t vocab) {
   l.part = kSortGroup;
   while ((uint64_t)n > (uint64_t)l.part * (10 * (l.part / kSortGroup))) l.part *= 2;
   l.sort_parts = (n + l.part - 1) / l.part;
-  const uint32_t vecs = (width + kVec - 1) / kVec;
+  const uint32_t vecs = (width + kLaneElements - 1) / kLaneElements;
   l.shift = std::max(std::min(next_power(vecs), 6u), kLeastShift);
   l.slabs = (vecs + 63) / 64;
   l.stride = l.slabs * 512;
   // Tiles: long, so that few sums cross one, as long as there is a wavefront for every SIMD four times.
-  l.tile = 128;
+  l.tile = 32;
   while (l.tile > 8 && (((uint64_t)n + l.tile - 1) / l.tile * l.slabs << l.shift) / 64 < 4096) l.tile /= 2;
   l.block = l.tile * (256u >> l.shift);
   l.blocks = (n + l.block - 1) / l.block;
@@ -125,18 +125,23 @@ int themis_embedding_lookup(const themis_rows_t* table, uint64_t vocab, uint64_t
   if (!table || !is_float_type(table->type) || (vocab && !rows_ok(table, false))) return THEMIS_ERR_INVALID_ARGUMENT;
   if (n > kMost || width > kMost || vocab > kMost) return THEMIS_ERR_UNSUPPORTED;
   if (!rows_apart(*out, n, width)) return THEMIS_ERR_INVALID_ARGUMENT;
-  const uint32_t vecs = (uint32_t)((width + kVec - 1) / kVec);
+  const uint32_t vecs = (uint32_t)((width + kLaneElements - 1) / kLaneElements);
   const uint32_t shift = std::min(next_power(vecs), 8u), chunks = (vecs + 255) / 256;
   if (chunks > 65535) return THEMIS_ERR_UNSUPPORTED;
   Launches go(stream);
   auto run = [&](auto kernel, uint32_t rows) {
     const uint64_t step = (256u >> shift) * rows;
     const uint32_t blocks = (uint32_t)std::min<uint64_t>((n + step - 1) / step, 1u << 20);
-    go(kernel, dim3(blocks, chunks), 256, *table, (uint32_t)vocab, (uint32_t)width, *ids, (uint32_t)n, scale, *out,
-       shift);
+    go(kernel, dim3(blocks, chunks), 256, rows_of(*table, vocab), (uint32_t)vocab, (uint32_t)width, rows_of(*ids, n),
+       (uint32_t)n, scale, rows_of(*out, n), shift);
   };
   with_type(table->type, [&](auto in) {
-    with_type(out->type, [&](auto to) { run(lookup_kernel<decltype(in), decltype(to), 1>, 1); });
+    with_type(out->type, [&](auto to) {
+      // Four rows a lane where that leaves a workgroup for every CU four times, and past the
+      // caches (65,536 rows of 4,096: 139 us, one row 180 us; 4,096 rows of 64: 3.1 and 2.2 us).
+      if (n / (256u >> shift) * chunks >= 4096) run(lookup_kernel<decltype(in), decltype(to), 4>, 4);
+      else run(lookup_kernel<decltype(in), decltype(to), 1>, 1);
+    });
   });
   return go.status();
 }
@@ -158,14 +163,26 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
   if (l.bytes && (!workspace || workspace_bytes < l.bytes || !aligned(workspace, 16))) return THEMIS_ERR_WORKSPACE;
   const uint64_t sums = (uint64_t)l.blocks * l.slabs;
   if (sums > 1u << 23 || l.slabs > 65535) return THEMIS_ERR_UNSUPPORTED;   // (grids of less than 2^32 lanes)
-  const themis_rows_t none = {nullptr, THEMIS_F32, 1, 0, 0};
-  const themis_rows_t g = n ? *grad_out : none, k = n ? *ids : none;
+  const Rows g = n ? rows_of(*grad_out, n) : Rows{}, k = n ? rows_of(*ids, n) : Rows{}, to = rows_of(*grad, vocab);
   const uint32_t skip = ignored >= 0 && (uint64_t)ignored < vocab ? (uint32_t)ignored : ~0u;
   Launches go(stream);
+  // (a workgroup's zeros: about 256 KiB, in up to 64 rows)
+  const uint32_t fill_rows = (uint32_t)std::min<uint64_t>(64, std::max<uint64_t>(1, (256u << 10) / (width * type_bytes(to.type))));
+  const uint64_t fill = accumulate ? 0 : std::min<uint64_t>((vocab + fill_rows - 1) / fill_rows, 1u << 20);
+  if (n <= kFewTokens) {
+    const uint32_t columns = (uint32_t)std::min<uint64_t>((width + 2047) / 2048, std::max<uint64_t>(1, 1024 / std::max<uint64_t>(n, 1)));
+    with_type(g.type, [&](auto in) {
+      with_type(to.type, [&](auto out) {
+        go(few_tokens_kernel<decltype(in), decltype(out)>, dim3((uint32_t)(n + fill), columns), 256, (uint32_t)n, g,
+           (uint32_t)width, k, scale, skip, accumulate != 0, to, (uint32_t)vocab, fill_rows);
+      });
+    });
+    return go.status();
+  }
   char* at = (char*)workspace;
   uint32_t *key[2] = {(uint32_t*)(at + l.key[0]), (uint32_t*)(at + l.key[1])};
   uint32_t *token[2] = {(uint32_t*)(at + l.token[0]), (uint32_t*)(at + l.token[1])};
-  for (uint32_t pass = 0; pass < l.passes && n; ++pass) {
+  for (uint32_t pass = 0; pass < l.passes; ++pass) {
     SortView s;
     s.n = (uint32_t)n;
     s.part = l.part;
@@ -181,8 +198,7 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
     go(sort_move_kernel, dim3(s.parts), kSortGroup, s, k, (uint32_t)vocab, skip);
   }
   TileView t;
-  t.key = key[(l.passes - 1) & 1];
-  t.token = token[(l.passes - 1) & 1];
+  const uint32_t *keys = key[(l.passes - 1) & 1], *tokens = token[(l.passes - 1) & 1];
   t.n = (uint32_t)n;
   t.tile = l.tile;
   t.block = l.block;
@@ -191,20 +207,18 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
   t.shift = l.shift;
   t.parts = (float*)(at + l.parts);
   t.stride = l.stride;
-  // (a workgroup's zeros: about 256 KiB, in up to 64 rows)
-  t.fill_rows = (uint32_t)std::min<uint64_t>(64, std::max<uint64_t>(1, (256u << 10) / (width * type_bytes(grad->type))));
-  const uint64_t fill = accumulate ? 0 : std::min<uint64_t>((vocab + t.fill_rows - 1) / t.fill_rows, 1u << 20);
+  t.fill_rows = fill_rows;
   with_type(g.type, [&](auto in) {
-    with_type(grad->type, [&](auto to) {
-      go(tile_sum_kernel<decltype(in), decltype(to)>, dim3((uint32_t)(sums + fill)), 256, t, g, (uint32_t)width,
-         scale, accumulate != 0, *grad, (uint32_t)vocab);
+    with_type(to.type, [&](auto out) {
+      typedef decltype(in) In;
+      typedef decltype(out) Out;
+      go(l.shift == 6 ? tile_sum_kernel<In, Out, true> : tile_sum_kernel<In, Out, false>, dim3((uint32_t)(sums + fill)),
+         256, t, keys, tokens, g, (uint32_t)width, scale, accumulate != 0, to, (uint32_t)vocab);
+      if (l.blocks > 1)
+        go(tile_join_kernel<kVecOf<In>, Out>, dim3(l.blocks - 1, l.slabs), 256, t, keys, (uint32_t)width, scale,
+           accumulate != 0, to, (uint32_t)vocab);
     });
   });
-  if (l.blocks > 1)
-    with_type(grad->type, [&](auto to) {
-      go(tile_join_kernel<decltype(to)>, dim3(l.blocks - 1, l.slabs), 256, t, (uint32_t)width, scale, accumulate != 0,
-         *grad, (uint32_t)vocab);
-    });
   return go.status();
 }
 

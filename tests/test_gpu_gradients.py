@@ -337,6 +337,80 @@ def test_grad_against_differences(gpu):
         assert abs(value(moved) - value(table) - want) <= (n + 4) * U * size
 
 
+@pytest.mark.parametrize("n", [4095, 4096, 4097, 4160, 8192, 9001])
+@pytest.mark.parametrize("width", [1, 9, 64, 65, 300, 777, 1032])
+def test_grad_on_both_sides_of_the_sort(gpu, n, width):
+    """Up to 4,096 tokens one launch, beyond a sort and tiles."""
+    vocab = 3000
+    g, ids = normal((n, width), BF16, n + width), numbers(n, vocab, I64, n, hot=0.1)
+    ids[::9] = vocab - 1
+    held = normal((vocab, width), F32, 8)
+    got = gpu.themis_embedding_grad(g.cuda(), ids.cuda(), vocab, 1.3, ignored=vocab - 1, out_dtype=F32)
+    check_grad(got, g, ids, vocab, 1.3, ignored=vocab - 1)
+    got = gpu.themis_embedding_grad(g.cuda(), ids.cuda(), vocab, 1.3, out=held.cuda(), accumulate=True)
+    check_grad(got, g, ids, vocab, 1.3, held=held)
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("to", [F32, BF16, F16])
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("width", [33, 520])
+def test_grad_types_of_many_tokens(gpu, width, kind, to, add):
+    n, vocab = 6000, 2500
+    g, ids = normal((n, width), kind, 1), numbers(n, vocab, I32, 2)
+    held = normal((vocab, width), to, 3) if add else None
+    got = gpu.themis_embedding_grad(g.cuda(), ids.cuda(), vocab, 0.7, ignored=int(ids[5]),
+                                    out=held.cuda() if add else None, out_dtype=to, accumulate=add)
+    check_grad(got, g, ids, vocab, 0.7, ignored=int(ids[5]), held=held)
+
+
+def test_grad_strides_of_many_tokens(gpu):
+    tokens, wide = numbers(90 * 81, 200, I64, 1).view(90, 81), normal((90, 81, 100), BF16, 2)
+    k, w = tokens.cuda(), wide.cuda()
+    for g, gg, ids, ii in ((wide[:, :-1, 3:90], w[:, :-1, 3:90], tokens[:, 1:], k[:, 1:]),
+                           (wide[:, :1].expand(90, 81, 100), w[:, :1].expand(90, 81, 100), tokens, k),
+                           (wide.transpose(0, 1), w.transpose(0, 1), tokens.t(), k.t())):
+        check_grad(gpu.themis_embedding_grad(gg, ii, 200, 1.5, out_dtype=F32), g, ids, 200, 1.5)
+    big = torch.full((400, 111), 5.0, device="cuda")
+    out = big[::2, 4:104]
+    assert gpu.themis_embedding_grad(w, k, 200, out=out) is out
+    check_grad(out, wide, tokens, 200, 1.0)
+    big[::2, 4:104] = 5.0
+    assert bool((big == 5.0).all())
+
+
+def test_grad_ignored_and_outside_among_many_tokens(gpu):
+    n, vocab, width = 9000, 60, 50
+    g, ids = normal((n, width), F32, 1), numbers(n, vocab, I64, 2)
+    ids[::7], ids[1::7], ids[2::7], ids[3::7] = -1, vocab, 2 ** 40, 17
+    g[(ids < 0) | (ids >= vocab) | (ids == 17)] = float("nan")
+    got = gpu.themis_embedding_grad(g.cuda(), ids.cuda(), vocab, 2.0, ignored=17)
+    check_grad(got, g, ids, vocab, 2.0, ignored=17)
+    held = normal((vocab, width), BF16, 3)
+    got = gpu.themis_embedding_grad(g.cuda(), ids.cuda(), vocab, 2.0, ignored=17, out=held.cuda(), accumulate=True)
+    check_grad(got, g, ids, vocab, 2.0, ignored=17, held=held)
+    ids[:] = 17
+    assert not gpu.themis_embedding_grad(g.cuda(), ids.cuda(), vocab, 2.0, ignored=17).any()
+    got = gpu.themis_embedding_grad(g.cuda(), ids.cuda(), vocab, 2.0, ignored=17, out=held.cuda(), accumulate=True)
+    same(got, held)
+
+
+def test_grad_workspace_of_many_tokens(gpu):
+    n, vocab, width = 20000, 900, 65
+    g, ids = normal((n, width), BF16, 3).cuda(), numbers(n, vocab, I64, 2, hot=0.2).cuda()
+    want = gpu.themis_embedding_grad(g, ids, vocab, out_dtype=F32)
+    need = gpu.themis_embedding_grad_workspace_bytes(n, width, vocab)
+    assert need > 0
+    for fill in (0, 0xFF, 0x7F):
+        work = torch.full((need + 64,), fill, dtype=torch.uint8, device="cuda")
+        same(gpu.themis_embedding_grad(g, ids, vocab, out_dtype=F32, workspace=work[:need]), want)
+        assert bool((work[need:] == fill).all())
+    for bad in (work[:need - 1], work[4:]):
+        with pytest.raises(gpu.ThemisError) as e:
+            gpu.themis_embedding_grad(g, ids, vocab, workspace=bad)
+        assert e.value.status == -4
+
+
 # -- norm and clipping --------------------------------------------------------------------
 
 def squares_64(grads):
