@@ -403,11 +403,11 @@ INVALID_ARGUMENT = -1
 def _rows(t: torch.Tensor, lead: int) -> Optional[_Rows]:
     """t as rows of its last dimension (lead = t.dim() - 1) or of single elements (lead =
     t.dim()), in the two levels of themis_rows; None where its strides need more."""
+    if t.is_contiguous():
+        return _Rows(t.data_ptr(), _TYPES[t.dtype], t.numel() or 1, 0,
+                     t.shape[-1] if lead < t.dim() else 1)
     if lead < t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
         return None
-    if t.is_contiguous():
-        step = t.shape[-1] if lead < t.dim() else 1
-        return _Rows(t.data_ptr(), _TYPES[t.dtype], max(1, t.numel()), 0, step)
     levels = []   # (rows, stride), outermost first, merged where one stride covers both
     for n, s in zip(t.shape[:lead], t.stride()[:lead]):
         if n == 1:
@@ -423,19 +423,6 @@ def _rows(t: torch.Tensor, lead: int) -> Optional[_Rows]:
     return _Rows(t.data_ptr(), _TYPES[t.dtype], max(1, inner), outer, step)
 
 
-def _need(ok: bool):
-    if not ok:
-        raise ThemisError(INVALID_ARGUMENT)
-
-
-def _is_float(t: torch.Tensor) -> bool:
-    return _TYPES.get(t.dtype, 9) < 3
-
-
-def _is_index(t: torch.Tensor) -> bool:
-    return t.dtype in (torch.int32, torch.int64)
-
-
 def _read_rows(t: torch.Tensor, lead: int) -> tuple:
     """(rows, the tensor that holds them): t itself, or a copy where its strides are beyond
     what the library reads."""
@@ -446,26 +433,48 @@ def _read_rows(t: torch.Tensor, lead: int) -> tuple:
     return r, t
 
 
+def _need(ok: bool):
+    if not ok:
+        raise ThemisError(INVALID_ARGUMENT)
+
+
+_FLOATS = frozenset((torch.float32, torch.bfloat16, torch.float16))
+_INDEXES = frozenset((torch.int32, torch.int64))
+
+
+def _stream_here(t: torch.Tensor) -> int:
+    """The current stream of t's GPU, which has to be the current one.  (Through the raw
+    handle: the stream object of torch.cuda.current_stream takes 2.7 us, a quarter of a call on
+    a few rows.)"""
+    device = t.get_device()
+    _need(device == torch._C._cuda_getDevice())
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def themis_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
                             out: Optional[torch.Tensor] = None,
                             out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """scale * table[ids] -> [*ids.shape, width] of out's type (given by out or out_dtype;
     the table's otherwise).  A token number outside the table gives a row of NaN."""
-    _need(table.dim() == 2 and _is_float(table) and _is_index(ids) and
-          table.device == ids.device and table.is_cuda)
+    _need(table.is_cuda and table.dim() == 2 and table.dtype in _FLOATS and ids.dtype in _INDEXES and
+          ids.get_device() == table.get_device())
     vocab, width = table.shape
+    shape = (*ids.shape, width)
     if out is None:
-        out = torch.empty((*ids.shape, width), dtype=out_dtype or table.dtype, device=table.device)
-    _need(_is_float(out) and out.shape == (*ids.shape, width) and out.device == table.device and
-          out_dtype in (None, out.dtype))
+        _need(out_dtype is None or out_dtype in _FLOATS)
+        out = table.new_empty(shape, dtype=out_dtype)
+    else:
+        _need(out.dtype in _FLOATS and out.shape == shape and out.device == table.device and
+              out_dtype in (None, out.dtype))
     n = ids.numel()
     if n == 0 or width == 0:
         return out
+    stream = _stream_here(table)
     rows_t, table = _read_rows(table, 1)
     rows_i, ids = _read_rows(ids, ids.dim())
     rows_o = _rows(out, out.dim() - 1)
     _need(rows_o is not None)
-    _check(lib().themis_embedding_lookup(rows_t, vocab, width, rows_i, n, scale, rows_o, _stream()))
+    _check(lib().themis_embedding_lookup(rows_t, vocab, width, rows_i, n, scale, rows_o, stream))
     return out
 
 
@@ -480,17 +489,21 @@ def themis_embedding_grad(grad_out: torch.Tensor, ids: torch.Tensor, vocab: int,
     """The gradient of the table behind themis_embedding_lookup -> [vocab, width] of out's type
     (given by out or out_dtype; grad_out's otherwise), or added to out where `accumulate`.
     Tokens of number `ignored`, or outside the table, have no gradient."""
-    _need(_is_float(grad_out) and _is_index(ids) and grad_out.shape[:-1] == ids.shape and
-          grad_out.dim() >= 1 and grad_out.device == ids.device and grad_out.is_cuda and
+    _need(grad_out.is_cuda and grad_out.dtype in _FLOATS and ids.dtype in _INDEXES and
+          grad_out.dim() >= 1 and grad_out.shape[:-1] == ids.shape and
+          ids.get_device() == grad_out.get_device() and
           vocab >= 0 and (out is not None or not accumulate))
     width = grad_out.shape[-1]
     if out is None:
-        out = torch.empty((vocab, width), dtype=out_dtype or grad_out.dtype, device=grad_out.device)
-    _need(_is_float(out) and out.shape == (vocab, width) and out.device == grad_out.device and
-          out_dtype in (None, out.dtype))
+        _need(out_dtype is None or out_dtype in _FLOATS)
+        out = grad_out.new_empty((vocab, width), dtype=out_dtype)
+    else:
+        _need(out.dtype in _FLOATS and out.shape == (vocab, width) and
+              out.device == grad_out.device and out_dtype in (None, out.dtype))
     n = ids.numel()
     if vocab == 0 or width == 0 or (n == 0 and accumulate):
         return out
+    stream = _stream_here(grad_out)
     rows_g, grad_out = _read_rows(grad_out, grad_out.dim() - 1)
     rows_i, ids = _read_rows(ids, ids.dim())
     rows_o = _rows(out, 1)
@@ -499,7 +512,7 @@ def themis_embedding_grad(grad_out: torch.Tensor, ids: torch.Tensor, vocab: int,
         workspace = alloc_workspace(themis_embedding_grad_workspace_bytes(n, width, vocab), out.device)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib().themis_embedding_grad(rows_g, width, rows_i, n, scale, ignored, int(accumulate),
-                                       rows_o, vocab, _ptr(workspace), ws_bytes, _stream()))
+                                       rows_o, vocab, _ptr(workspace), ws_bytes, stream))
     return out
 
 
@@ -518,6 +531,10 @@ class GradientPlan:
     @property
     def device(self):
         return self.image.device
+
+    @property
+    def workspace_at(self) -> Optional[int]:
+        return None if self.workspace is None else self.workspace.data_ptr()
 
 
 def _views(g: torch.Tensor, o: Optional[torch.Tensor]):
@@ -549,11 +566,11 @@ def themis_gradient_plan(grads, out=None) -> GradientPlan:
     types (parts of a flat bucket, say); the gradients themselves where it is not given.  Good
     for as long as the tensors stay where they are; their values may change."""
     grads = list(grads)
-    _need(all(_is_float(g) and g.is_cuda for g in grads) and
+    _need(all(g.dtype in _FLOATS and g.is_cuda for g in grads) and
           len({g.device for g in grads}) <= 1)
     outs = grads if out is None else list(out)
     _need(len(outs) == len(grads) and
-          all(_is_float(o) and o.shape == g.shape and o.device == g.device for g, o in zip(grads, outs)))
+          all(o.dtype in _FLOATS and o.shape == g.shape and o.device == g.device for g, o in zip(grads, outs)))
     # (a gradient that is its own target and has elements in one place cannot be scaled there:
     # then only its norm is to be had)
     no_out = out is None and any(s == 0 and n > 1 for g in grads for n, s in zip(g.shape, g.stride()))
@@ -580,18 +597,18 @@ def themis_gradient_plan(grads, out=None) -> GradientPlan:
 
 def themis_gradient_norm(plan: GradientPlan):
     """Euclidean norms -> (total f32[1], norms f32[n_tensors])."""
-    result = torch.empty(1 + plan.n_tensors, dtype=torch.float32, device=plan.device)
-    total, norms = result[:1], result[1:]
-    _check(lib().themis_gradient_norm(plan.c_struct, total.data_ptr(), norms.data_ptr(),
-                                      _ptr(plan.workspace), plan.c_struct.workspace_bytes, _stream()))
-    return total, norms
+    result = plan.image.new_empty(1 + plan.n_tensors, dtype=torch.float32)
+    at = result.data_ptr()
+    _check(lib().themis_gradient_norm(plan.c_struct, at, at + 4, plan.workspace_at,
+                                      plan.c_struct.workspace_bytes, _stream_here(plan.image)))
+    return result.split((1, plan.n_tensors))
 
 
 def themis_gradient_clip(plan: GradientPlan, max_norm: float):
     """The same, and the gradients times min(1, max_norm / norm) into the plan's targets
     -> (f32[2]: norm and factor, norms f32[n_tensors])."""
-    result = torch.empty(2 + plan.n_tensors, dtype=torch.float32, device=plan.device)
-    total, norms = result[:2], result[2:]
-    _check(lib().themis_gradient_clip(plan.c_struct, float(max_norm), total.data_ptr(), norms.data_ptr(),
-                                      _ptr(plan.workspace), plan.c_struct.workspace_bytes, _stream()))
-    return total, norms
+    result = plan.image.new_empty(2 + plan.n_tensors, dtype=torch.float32)
+    at = result.data_ptr()
+    _check(lib().themis_gradient_clip(plan.c_struct, max_norm, at, at + 8, plan.workspace_at,
+                                      plan.c_struct.workspace_bytes, _stream_here(plan.image)))
+    return result.split((2, plan.n_tensors))
