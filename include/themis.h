@@ -588,6 +588,7 @@ typedef struct themis_gradient_plan {
   uint64_t n_pieces;
   uint64_t image_bytes;
   uint64_t workspace_bytes; /* of themis_gradient_norm / _clip              */
+  uint64_t in_bytes;        /* of all elements                              */
   uint32_t has_out;         /* every part has an out                        */
   uint32_t strided;         /* some part is not one run of adjacent elements */
   const void *image;        /* device copy of the image                     */

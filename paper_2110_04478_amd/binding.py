@@ -47,7 +47,7 @@ class _Gradient(C.Structure):
 
 class _GradientPlan(C.Structure):
     _fields_ = [("n_tensors", C.c_uint64), ("n_pieces", C.c_uint64), ("image_bytes", C.c_uint64),
-                ("workspace_bytes", C.c_uint64), ("has_out", C.c_uint32), ("strided", C.c_uint32),
+                ("workspace_bytes", C.c_uint64), ("in_bytes", C.c_uint64), ("has_out", C.c_uint32), ("strided", C.c_uint32),
                 ("image", _vp)]
 
 

@@ -9,26 +9,33 @@
 
 #include "themis_elements.hpp"
 
-#ifndef CL
-#define CL load_once
-#endif
-#ifndef CS
-#define CS store_away
-#endif
-#ifndef NL
-#define NL load
-#endif
-#ifndef NG
-#define NG 2048
-#endif
-#ifndef PM
-#define PM 65536
-#endif
 namespace themis {
 
 constexpr uint32_t kPieceLeast = 2048;   // one access of 256 lanes
-constexpr uint32_t kPieceMost = PM;
-constexpr uint32_t kNormGroups = NG;   // workgroups of a pass over the list: eight for every CU
+constexpr uint32_t kPieceMost = 65536;
+constexpr uint32_t kInFlight = 8;        // accesses of a lane
+
+// Workgroups of a pass over the list: four for every CU, two where the list is long and each has
+// many pieces (1.07 G binary32 elements clipped into bf16 1,727 us, with four 1,770; 16.8 M bf16
+// 36 and 31 us).
+__host__ __device__ inline uint32_t pass_groups(uint32_t n_pieces) {
+  const uint32_t most = n_pieces > 8192 ? 512 : 1024;
+  return n_pieces < most ? n_pieces : most;
+}
+// Elements of a piece: one for every workgroup while that keeps its lanes' accesses in flight, then
+// eight for every workgroup, so that they end together.
+inline uint64_t piece_elements(uint64_t total) {
+  const uint64_t one = total / 1024 < 16384 ? total / 1024 : 16384;
+  const uint64_t eight = total / 8192 < kPieceMost ? total / 8192 : kPieceMost;
+  const uint64_t some = one > eight ? one : eight;
+  return some <= kPieceLeast ? kPieceLeast : (some + kPieceLeast - 1) / kPieceLeast * kPieceLeast;
+}
+
+// The last cache level holds 256 MiB: of a list that is longer, all but its last part is read past
+// it in the first pass, so that the part the second pass begins with is still there (clip of 1.07 G
+// binary32 elements 1,798 -> 1,773 us, of 134 M bf16 elements 144 -> 137 us; nothing past it:
+// 1,873 and 138 us; the norm of 1.74 G bf16 elements 583 -> 514 us).
+constexpr uint64_t kKeptBytes = 192ull << 20;
 
 enum : uint32_t { kInDense = 1u << 16, kOutDense = 1u << 17, kInPlace = 1u << 18 };
 
@@ -54,10 +61,7 @@ inline PlanView plan_view(const themis_gradient_plan_t& p) {
           (uint32_t)p.n_pieces, (uint32_t)p.n_tensors};
 }
 
-// The workspace: the workgroups' sums of squares, then the pieces'.
-__host__ __device__ inline uint32_t norm_groups(uint32_t n_pieces) {
-  return n_pieces < kNormGroups ? n_pieces : kNormGroups;
-}
+// The workspace: the workgroups' sums of squares (pass_groups()), then the pieces'.
 
 // ---------------------------------------------------------------------------
 // Sums over a workgroup of 256 lanes, the same in every lane.
@@ -86,19 +90,19 @@ __device__ __forceinline__ double squares(Floats<N> v, double sum) {
   return sum + odd;
 }
 
-// A lane's share of a piece's sum of squares.
-template <typename T>
+// A lane's share of a piece's sum of squares; kOnce: read past the caches.
+template <bool kOnce, typename T>
 __device__ __forceinline__ double piece_squares(const Piece& p) {
   const T* in = (const T*)p.in;
   double sum = 0.0;
   if (p.kind & kInDense) {
     constexpr int kVec = kVecOf<T>;
-    constexpr uint32_t kStep = 256 * kVec, kUnroll = 4;
+    constexpr uint32_t kStep = 256 * kVec, kUnroll = kInFlight;
     uint32_t e = threadIdx.x * kVec;
     for (; e + (kUnroll - 1) * kStep + kVec <= p.count; e += kUnroll * kStep) {
       typename Packed<T, kVec>::type v[kUnroll];
 #pragma unroll
-      for (uint32_t k = 0; k < kUnroll; ++k) v[k] = NL<kVec>(in + e + k * kStep);
+      for (uint32_t k = 0; k < kUnroll; ++k) v[k] = kOnce ? load_once<kVec>(in + e + k * kStep) : load<kVec>(in + e + k * kStep);
 #pragma unroll
       for (uint32_t k = 0; k < kUnroll; ++k) sum = squares<kVec>(widen<kVec>(v[k]), sum);
     }
@@ -114,15 +118,20 @@ __device__ __forceinline__ double piece_squares(const Piece& p) {
   return sum;
 }
 
+template <bool kOnce>
+__device__ __forceinline__ double piece_squares_of(const Piece& p) {
+  const uint32_t type = p.kind & 0xffu;
+  return type == THEMIS_F32 ? piece_squares<kOnce, float>(p)
+         : type == THEMIS_BF16 ? piece_squares<kOnce, __bf16>(p) : piece_squares<kOnce, _Float16>(p);
+}
+
 __global__ void __launch_bounds__(256)
-norm_kernel(PlanView plan, double* __restrict__ group_sums, double* __restrict__ piece_sums) {
+norm_kernel(PlanView plan, uint32_t passed, double* __restrict__ group_sums, double* __restrict__ piece_sums) {
   __shared__ double part[4];
   double total = 0.0;
   for (uint32_t i = blockIdx.x; i < plan.n_pieces; i += gridDim.x) {
     const Piece& p = plan.pieces[i];
-    const uint32_t type = p.kind & 0xffu;
-    double s = type == THEMIS_F32 ? piece_squares<float>(p)
-               : type == THEMIS_BF16 ? piece_squares<__bf16>(p) : piece_squares<_Float16>(p);
+    double s = i < passed ? piece_squares_of<true>(p) : piece_squares_of<false>(p);
     s = group_sum(s, part);
     total += s;
     if (threadIdx.x == 0) piece_sums[i] = s;
@@ -164,14 +173,14 @@ __device__ __forceinline__ void scale_piece(const Piece& p, float factor) {
   Out* out = (Out*)p.out;
   if ((p.kind & (kInDense | kOutDense)) == (kInDense | kOutDense)) {
     constexpr int kVec = kVecOf<In, Out>;
-    constexpr uint32_t kStep = 256 * kVec, kUnroll = 4;
+    constexpr uint32_t kStep = 256 * kVec, kUnroll = kInFlight;
     uint32_t e = threadIdx.x * kVec;
     for (; e + (kUnroll - 1) * kStep + kVec <= p.count; e += kUnroll * kStep) {
       typename Packed<In, kVec>::type v[kUnroll];
 #pragma unroll
-      for (uint32_t k = 0; k < kUnroll; ++k) v[k] = CL<kVec>(in + e + k * kStep);
+      for (uint32_t k = 0; k < kUnroll; ++k) v[k] = load_once<kVec>(in + e + k * kStep);
 #pragma unroll
-      for (uint32_t k = 0; k < kUnroll; ++k) CS<kVec>(out + e + k * kStep, widen<kVec>(v[k]) * factor);
+      for (uint32_t k = 0; k < kUnroll; ++k) store_away<kVec>(out + e + k * kStep, widen<kVec>(v[k]) * factor);
     }
     for (; e < p.count; e += kStep) {
       const uint32_t some = min(p.count - e, (uint32_t)kVec);

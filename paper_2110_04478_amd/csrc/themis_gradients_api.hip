@@ -227,6 +227,7 @@ int themis_gradient_plan(const themis_gradient_t* parts, uint64_t n_parts, uint6
   if (!plan || (n_parts && !parts)) return THEMIS_ERR_INVALID_ARGUMENT;
   if (n_tensors > kMostTensors) return THEMIS_ERR_UNSUPPORTED;
   unsigned __int128 total = 0;
+  uint64_t bytes = 0;
   bool has_out = true, strided = false;
   for (uint64_t i = 0; i < n_parts; ++i) {
     const themis_gradient_t& g = parts[i];
@@ -243,12 +244,10 @@ int themis_gradient_plan(const themis_gradient_t* parts, uint64_t n_parts, uint6
       return THEMIS_ERR_INVALID_ARGUMENT;   // (an element written twice)
     has_out = has_out && g.out;
     total += count;
+    bytes += (uint64_t)count * type_bytes(g.in_type);
   }
   if (total >> 46) return THEMIS_ERR_UNSUPPORTED;
-  // Pieces: small where the list is, so that it reaches all CUs, and of one size in multiples of
-  // what a workgroup takes at a time.
-  uint64_t most = ((uint64_t)total / (2 * kNormGroups) + kPieceLeast - 1) / kPieceLeast * kPieceLeast;
-  most = std::min<uint64_t>(std::max<uint64_t>(most, kPieceLeast), kPieceMost);
+  const uint64_t most = piece_elements((uint64_t)total);
 
   uint64_t n_pieces = 0;
   Piece* to = (Piece*)image;
@@ -299,7 +298,8 @@ int themis_gradient_plan(const themis_gradient_t* parts, uint64_t n_parts, uint6
   plan->n_tensors = n_tensors;
   plan->n_pieces = n_pieces;
   plan->image_bytes = room;
-  plan->workspace_bytes = (norm_groups((uint32_t)n_pieces) + n_pieces) * sizeof(double);
+  plan->workspace_bytes = (pass_groups((uint32_t)n_pieces) + n_pieces) * sizeof(double);
+  plan->in_bytes = bytes;
   plan->has_out = has_out;
   plan->strided = strided;
   plan->image = nullptr;
@@ -315,7 +315,7 @@ static int gradient_pass(const themis_gradient_plan_t* plan, double max_norm, bo
   if (!plan || !plan->image || !total || !aligned(plan->image, 16)) return THEMIS_ERR_INVALID_ARGUMENT;
   if (plan->n_pieces >= kMost || plan->n_tensors > kMostTensors) return THEMIS_ERR_UNSUPPORTED;
   if (clip && (!(max_norm > 0.0) || !std::isfinite(max_norm) || !plan->has_out)) return THEMIS_ERR_INVALID_ARGUMENT;
-  const uint32_t groups = norm_groups((uint32_t)plan->n_pieces);
+  const uint32_t groups = pass_groups((uint32_t)plan->n_pieces);
   const size_t need = (groups + plan->n_pieces) * sizeof(double);
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return THEMIS_ERR_WORKSPACE;
   const PlanView view = plan_view(*plan);
@@ -323,7 +323,9 @@ static int gradient_pass(const themis_gradient_plan_t* plan, double max_norm, bo
   double* piece_sums = group_sums + groups;
   const uint32_t norm_blocks = norms ? (uint32_t)((plan->n_tensors + 3) / 4) : 0u;
   Launches go(stream);
-  if (groups) go(norm_kernel, dim3(groups), 256, view, group_sums, piece_sums);
+  const uint32_t passed = plan->in_bytes <= kKeptBytes ? 0u
+                          : (uint32_t)((double)plan->n_pieces * (1.0 - (double)kKeptBytes / (double)plan->in_bytes));
+  if (groups) go(norm_kernel, dim3(groups), 256, view, passed, group_sums, piece_sums);
   if (clip) {
     const uint32_t scalers = std::max(groups, 1u);
     go(clip_kernel, dim3(scalers + norm_blocks), 256, view, groups, group_sums, piece_sums, max_norm, scalers, total,
