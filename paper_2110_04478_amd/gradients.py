@@ -1,0 +1,81 @@
+"""Between torch.autograd, the gradient operators and the evaluator's traces: a
+token table whose gradient the library sums, and the flat buckets that an
+iteration's collectives carry."""
+from __future__ import annotations
+
+from typing import Optional
+
+import numpy as np
+import torch
+
+from . import binding
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, scale, ignored, into):
+        ctx.save_for_backward(ids)
+        ctx.args = (table.shape[0], table.dtype, scale, ignored, into)
+        return binding.themis_embedding_lookup(table, ids, scale)
+
+    @staticmethod
+    def backward(ctx, grad_out):
+        (ids,) = ctx.saved_tensors
+        vocab, dtype, scale, ignored, into = ctx.args
+        if into is not None:
+            binding.themis_embedding_grad(grad_out, ids, vocab, scale, ignored, out=into, accumulate=True)
+            return None, None, None, None, None
+        grad = binding.themis_embedding_grad(grad_out, ids, vocab, scale, ignored, out_dtype=dtype)
+        return grad, None, None, None, None
+
+
+def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, ignored: int = -1,
+              into: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """scale * table[ids], differentiable in the table; tokens of number `ignored` have no gradient.
+
+    into: where the gradient is added in place of being returned to autograd (table.grad, say: a
+    table that is also the output projection has one already, and only the rows of the tokens at
+    hand are touched)."""
+    return _Embedding.apply(table, ids, float(scale), int(ignored), into)
+
+
+class GradientBuckets:
+    """The gradients of a list of parameters, and the flat buckets that carry them.
+
+    Every parameter gets a .grad of zeros that stays where it is (use zero(), not
+    zero_grad(set_to_none=True)); the buckets are filled in the order in which gradients become
+    ready, the last parameter's first, each with at least bucket_bytes unless it is the last."""
+
+    def __init__(self, params, bucket_bytes: int, dtype: torch.dtype = torch.bfloat16):
+        self.params = [p for p in params if p.requires_grad]
+        if not self.params:
+            raise binding.ThemisError(binding.INVALID_ARGUMENT)
+        self.buckets, groups, size = [], [[]], 0
+        for p in reversed(self.params):
+            p.grad = torch.zeros_like(p, memory_format=torch.contiguous_format)
+            if size >= bucket_bytes:
+                groups.append([])
+                size = 0
+            groups[-1].append(p)
+            size += p.numel() * dtype.itemsize
+        self.views = {}
+        for group in groups:
+            flat = torch.zeros(sum(p.numel() for p in group), dtype=dtype, device=group[0].device)
+            for p, part in zip(group, flat.split([p.numel() for p in group])):
+                self.views[p] = part.view(p.shape)
+            self.buckets.append(flat)
+        self.plan = binding.themis_gradient_plan([p.grad for p in self.params],
+                                                 [self.views[p] for p in self.params])
+
+    def zero(self):
+        for p in self.params:
+            p.grad.zero_()
+
+    def clip(self, max_norm: float):
+        """The clipped gradients into the buckets -> (f32[2]: norm and factor, norms of the
+        parameters' gradients f32[n])."""
+        return binding.themis_gradient_clip(self.plan, max_norm)
+
+    def sizes(self) -> np.ndarray:
+        """Bytes of the buckets: the collectives of an iteration, in the order of their issue."""
+        return np.array([b.numel() * b.element_size() for b in self.buckets], dtype=np.float64)
