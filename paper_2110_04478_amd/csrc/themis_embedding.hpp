@@ -82,8 +82,10 @@ __device__ __forceinline__ float8 sum_listed(const Slice<kVec>& slice, const Row
   return sum;
 }
 
-// Zeros in the rows of `empty` behind v0, by a workgroup: short rows side by side.
-template <typename Out>
+// Zeros in the rows of `empty` behind v0, by a workgroup: short rows side by side.  kAway: past the
+// caches (beside sums that need them: 65,537 tokens of 1,000 108 us, through them 116; alone it is
+// 200 MB in 52 us and 45).
+template <bool kAway, typename Out>
 __device__ __forceinline__ void write_zeros(uint64_t empty, uint32_t v0, uint32_t width, const Rows& grad) {
   constexpr int kVec = kVecOf<Out>;
   const uint32_t vecs = (width + kVec - 1) / kVec;
@@ -91,9 +93,37 @@ __device__ __forceinline__ void write_zeros(uint64_t empty, uint32_t v0, uint32_
   for (uint32_t r = threadIdx.x >> shift; r < 64; r += 256u >> shift) {
     if (!((empty >> r) & 1u)) continue;
     Out* to = row_at<Out>(grad, v0 + r);
-    for (uint32_t c = threadIdx.x & ((1u << shift) - 1u); c < vecs; c += 256)
-      store_some_away<kVec>(to + c * kVec, Floats<kVec>(0.0f), min(width - c * kVec, (uint32_t)kVec));
+    for (uint32_t c = threadIdx.x & ((1u << shift) - 1u); c < vecs; c += 256) {
+      const uint32_t count = min(width - c * kVec, (uint32_t)kVec);
+      if (kAway) store_some_away<kVec>(to + c * kVec, Floats<kVec>(0.0f), count);
+      else store_some<kVec>(to + c * kVec, Floats<kVec>(0.0f), count);
+    }
   }
+}
+
+// Zeros in a whole table, before the sums.  One store a lane: workgroups that end at once follow each
+// other through memory, and nothing is waited for (1 GiB: 7.1 TB/s; in loops over 16 KiB to 1 MiB, or
+// behind a look at whether a row is needed, 4 to 6).
+__global__ void __launch_bounds__(256) clear_kernel(char* table, uint64_t bytes) {
+  const uint64_t head = min((uint64_t)(-(uintptr_t)table & 15u), bytes), body = (bytes - head) / 16;
+  uint4* to = (uint4*)(table + head);
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < body; i += (uint64_t)gridDim.x * 256)
+    to[i] = make_uint4(0, 0, 0, 0);
+  if (blockIdx.x) return;   // what is not aligned to 16 bytes
+  if (threadIdx.x < head) table[threadIdx.x] = 0;
+  const uint64_t rest = head + body * 16 + threadIdx.x;
+  if (rest < bytes) table[rest] = 0;
+}
+// The same, rows that do not follow each other: 2^shift lanes a row, or 4 KiB of one.
+template <typename Out>
+__global__ void __launch_bounds__(256)
+clear_rows_kernel(Rows table, uint32_t width, uint32_t vocab, uint32_t shift) {
+  constexpr uint32_t kVec = kVecOf<Out>;
+  for (uint64_t c = ((uint64_t)blockIdx.y * 256u + (threadIdx.x & ((1u << shift) - 1u))) * kVec; c < width;
+       c += (uint64_t)gridDim.y * 256u * kVec)
+    for (uint64_t v = (uint64_t)blockIdx.x * (256u >> shift) + (threadIdx.x >> shift); v < vocab;
+         v += (uint64_t)gridDim.x * (256u >> shift))
+      store_some<kVec>(row_at<Out>(table, (uint32_t)v) + c, Floats<kVec>(0.0f), min(width - (uint32_t)c, kVec));
 }
 
 template <bool kFull, int kVec, typename Out>
@@ -133,7 +163,7 @@ few_tokens_kernel(uint32_t n, Rows grad_out, uint32_t width, Rows ids, float sca
       }
       __syncthreads();
       const uint64_t all = rows == 64 ? ~0ull : (1ull << rows) - 1;
-      write_zeros<Out>(all & ~masks[0], v0, width, grad);
+      write_zeros<false, Out>(all & ~masks[0], v0, width, grad);
     }
     return;
   }
@@ -370,7 +400,7 @@ __device__ __forceinline__ void fill_rows(const TileView& s, const uint32_t* key
       else hi = mid;
     }
   }
-  write_zeros<Out>(__ballot(mine && (lo >= s.n || keys[lo] != v)), v0, width, grad);
+  write_zeros<true, Out>(__ballot(mine && (lo >= s.n || keys[lo] != v)), v0, width, grad);
 }
 
 // A tile's sums: those that begin and end in it to the table, the others to `head` (one that began

@@ -111,6 +111,31 @@ GradLayout grad_layout(uint32_t n, uint32_t width, uint32_t vocab) {
   return l;
 }
 
+void clear_table(Launches& go, const Rows& table, uint32_t width, uint32_t vocab) {
+  if (table.inner == 0 && table.inner_stride == (int64_t)width) {
+    const uint64_t bytes = (uint64_t)vocab * width * type_bytes(table.type);
+    go(clear_kernel, dim3((uint32_t)std::min<uint64_t>((bytes + 4095) / 4096, (1u << 24) - 1)), 256, table.data, bytes);
+    return;
+  }
+  const uint32_t vec = table.type == THEMIS_F32 ? 4 : 8, vecs = (width + vec - 1) / vec;
+  const uint32_t shift = std::min(next_power(vecs), 8u), rows = 256u >> shift;
+  with_type(table.type, [&](auto out) {
+    go(clear_rows_kernel<decltype(out)>, dim3(std::min((vocab + rows - 1) / rows, (1u << 24) - 1), std::min((vecs + 255) / 256, 65535u)), 256,
+       table, width, vocab, shift);
+  });
+}
+
+// Whether zeros are written by a launch of their own before the sums, in all rows, or with the sums
+// in those rows that no token has.  The first is the faster store, but writes the rows of the sums
+// twice.  One token, 16 MiB: 9 us with the sums, 8 and another launch before; 128 MiB: 27 and 25;
+// 1 GiB: 195 and 161.  16,384 tokens, 1 GiB in 131,072 rows: 246 and 235 us; 512 MiB in 65,536 rows:
+// 145 and 162.  Rows that end inside a line share it with the next, whose zeros another workgroup
+// writes: 16,384 tokens, 131 MB in 65,537 rows of 2,002 bytes 73 and 61 us, 65,536 tokens 89 and 107.
+bool clears(uint64_t n, uint64_t vocab, uint64_t width, int type) {
+  const uint64_t row = width * type_bytes(type), least = row % 128 ? 2 : 8;
+  return n == 0 || (vocab * row > 64u << 20 && (n <= kFewTokens || vocab >= least * n));
+}
+
 }  // namespace
 }  // namespace themis
 
@@ -168,7 +193,10 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
   Launches go(stream);
   // (a workgroup's zeros: about 256 KiB, in up to 64 rows)
   const uint32_t fill_rows = (uint32_t)std::min<uint64_t>(64, std::max<uint64_t>(1, (256u << 10) / (width * type_bytes(to.type))));
-  const uint64_t fill = accumulate ? 0 : std::min<uint64_t>((vocab + fill_rows - 1) / fill_rows, 1u << 20);
+  const bool clear = !accumulate && clears(n, vocab, width, to.type);
+  const uint64_t fill = accumulate || clear ? 0 : std::min<uint64_t>((vocab + fill_rows - 1) / fill_rows, 1u << 20);
+  if (clear) clear_table(go, to, (uint32_t)width, (uint32_t)vocab);
+  if (n == 0) return go.status();
   if (n <= kFewTokens) {
     const uint32_t columns = (uint32_t)std::min<uint64_t>((width + 2047) / 2048, std::max<uint64_t>(1, 1024 / std::max<uint64_t>(n, 1)));
     with_type(g.type, [&](auto in) {
