@@ -78,8 +78,8 @@ __device__ __forceinline__ void store_some_away(T* p, Floats<N> v, uint32_t coun
 
 // Eight elements of a row for every lane of a group of `lanes`, `first` being the group's first:
 // adjacent ones (kVec = 8), or four and four, `lanes` accesses apart (kVec = 4).  Only the last ones
-// of a row may be short of eight: code that keeps loads in flight has a copy for full() lanes, in
-// which no access depends on a count.
+// of a row may be short of that: code that keeps loads in flight has a copy for full() lanes, whose
+// accesses are whole, and in which no load depends on a count.
 template <int kVec>
 struct Slice;
 template <>
@@ -114,9 +114,10 @@ struct Slice<4> {
     next = at + lanes * 4;
     count = at < width ? min(width - at, 4u) : 0u;
     more = next < width ? min(width - next, 4u) : 0u;
+    if (!more) next = at;   // (what is read there is not used)
   }
   __device__ __forceinline__ bool any() const { return count != 0; }
-  __device__ __forceinline__ bool full() const { return more == 4; }
+  __device__ __forceinline__ bool full() const { return count == 4 && (more & 3u) == 0; }
   template <bool kFull, typename T>
   __device__ __forceinline__ typename Packed<T, 8>::type read(const T* row) const {
     const auto a = kFull ? load<4>(row + at) : load_some<4>(row + at, count);
@@ -127,7 +128,7 @@ struct Slice<4> {
   __device__ __forceinline__ void write(T* row, float8 v) const {
     if (kFull) {
       store<4>(row + at, v.lo);
-      store<4>(row + next, v.hi);
+      if (more) store<4>(row + next, v.hi);
     } else {
       store_some<4>(row + at, v.lo, count);
       store_some<4>(row + next, v.hi, more);
@@ -137,7 +138,7 @@ struct Slice<4> {
   __device__ __forceinline__ void write_away(T* row, float8 v) const {
     if (!kFull) return write<false>(row, v);
     store_away<4>(row + at, v.lo);
-    store_away<4>(row + next, v.hi);
+    if (more) store_away<4>(row + next, v.hi);
   }
 };
 constexpr uint32_t kLaneElements = 8;

@@ -490,7 +490,7 @@ tile_sum_kernel(TileView s, const uint32_t* __restrict__ keys, const uint32_t* _
   const uint32_t shift = kWave ? 6u : s.shift, lanes = 1u << shift;
   const uint32_t block = number / s.slabs, slab = number - block * s.slabs;
   const uint32_t group = kWave ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x >> shift;
-  constexpr int kVec = kVecOf<In>;
+  constexpr int kVec = kVecOf<In, Out>;
   const Slice<kVec> slice(slab * 512u, threadIdx.x & (lanes - 1u), lanes, width);
   const uint32_t block_end = min(block * s.block + s.block, s.n);
   const uint32_t first = block * s.block + group * s.tile, last = min(first + s.tile, s.n);

@@ -243,7 +243,7 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
       go(l.shift == 6 ? tile_sum_kernel<In, Out, true> : tile_sum_kernel<In, Out, false>, dim3((uint32_t)(sums + fill)),
          256, t, keys, tokens, g, (uint32_t)width, scale, accumulate != 0, to, (uint32_t)vocab);
       if (l.blocks > 1)
-        go(tile_join_kernel<kVecOf<In>, Out>, dim3(l.blocks - 1, l.slabs), kJoinWaves * 64, t, keys, (uint32_t)width, scale,
+        go(tile_join_kernel<kVecOf<In, Out>, Out>, dim3(l.blocks - 1, l.slabs), kJoinWaves * 64, t, keys, (uint32_t)width, scale,
            accumulate != 0, to, (uint32_t)vocab);
     });
   });
