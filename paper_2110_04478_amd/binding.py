@@ -571,20 +571,26 @@ def themis_gradient_plan(grads, out=None) -> GradientPlan:
     outs = grads if out is None else list(out)
     _need(len(outs) == len(grads) and
           all(o.dtype in _FLOATS and o.shape == g.shape and o.device == g.device for g, o in zip(grads, outs)))
-    # (a gradient that is its own target and has elements in one place cannot be scaled there:
-    # then only its norm is to be had)
-    no_out = out is None and any(s == 0 and n > 1 for g in grads for n, s in zip(g.shape, g.stride()))
-    parts = []
-    for i, (g, o) in enumerate(zip(grads, outs)):
-        if g.numel() == 0:
-            continue
-        gt, ot, ge, oe = _TYPES[g.dtype], _TYPES[o.dtype], g.element_size(), o.element_size()
-        for x, y, rows, cols, ra, ca, rb, cb in _views(g, o):
-            parts.append(_Gradient(g.data_ptr() + x * ge, None if no_out else o.data_ptr() + y * oe, i,
-                                   gt, ot, rows, cols, ra, ca, rb, cb))
-    array = (_Gradient * len(parts))(*parts)
+    # (gradients that are their own targets and share elements, a broadcast or one given twice,
+    # cannot be scaled in place: then only norms are to be had)
+    places = [(o.data_ptr(), tuple(o.shape), o.stride()) for o in outs if o.numel()]
+    twice = len(places) != len(set(places))
+    _need(out is None or not twice)
     plan = _GradientPlan()
-    _check(lib().themis_gradient_plan(array, len(parts), len(grads), plan, None, 0))
+    for with_out in ((False,) if twice else (True, False) if out is None else (True,)):
+        parts = []
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            if g.numel() == 0:
+                continue
+            gt, ot, ge, oe = _TYPES[g.dtype], _TYPES[o.dtype], g.element_size(), o.element_size()
+            for x, y, rows, cols, ra, ca, rb, cb in _views(g, o):
+                parts.append(_Gradient(g.data_ptr() + x * ge, o.data_ptr() + y * oe if with_out else None, i,
+                                       gt, ot, rows, cols, ra, ca, rb, cb))
+        array = (_Gradient * len(parts))(*parts)
+        status = lib().themis_gradient_plan(array, len(parts), len(grads), plan, None, 0)
+        if status != INVALID_ARGUMENT:
+            break
+    _check(status)
     image = np.empty((plan.image_bytes + 7) // 8, dtype=np.uint64)
     _check(lib().themis_gradient_plan(array, len(parts), len(grads), plan, image.ctypes.data,
                                       image.nbytes))

@@ -11,7 +11,9 @@ namespace themis {
 // 2^shift lanes take a row (a chunk of 2,048 elements of a longer one: blockIdx.y), each eight
 // elements; a workgroup of 256 lanes takes kRows rows per group of lanes at once, so that their
 // loads are in flight together: the number, then the row, are two dependent trips to memory and
-// all that there is to hide.
+// all that there is to hide.  Bound by memory: 65,536 rows of 4,096 bf16 (0.70 GB with each table row
+// once) in 133 us, 5.3 TB/s, where a copy of 4 GiB makes 4.8 and one of 128 MiB 7.2; a few rows take
+// the time of a launch.
 // ---------------------------------------------------------------------------
 template <bool kFull, int kRows, typename In, typename Out, int kVec>
 __device__ __forceinline__ void lookup_rows(const Slice<kVec>& slice, const Rows& table, uint32_t vocab, const Rows& ids,
@@ -57,7 +59,10 @@ lookup_kernel(Rows table, uint32_t vocab, uint32_t width, Rows ids, uint32_t n, 
 // Up to kFewTokens tokens: one launch, no workspace.  A workgroup for every token finds all tokens
 // of its number; the workgroups of one number share the row's elements (a token that occurs often
 // has many), and the lanes of a workgroup the elements and the tokens: G groups of lanes take a
-// G-th of the tokens each, in order, and their sums are added in order.
+// G-th of the tokens each, in order, and their sums are added in order.  Bound by the waits one after
+// the other (number, numbers, rows, what they are added to) and, towards kFewTokens, by every
+// workgroup's look at all numbers: added to a binary32 table, rows of 1,024, 512 tokens 5.4 us, 2,048
+// 10.9, 4,096 23.5, where the sort below takes 20, 23 and 26.
 // ---------------------------------------------------------------------------
 constexpr uint32_t kFewTokens = 4096;
 constexpr uint32_t kRowsInFlight = 8;
@@ -146,7 +151,8 @@ few_tokens_kernel(uint32_t n, Rows grad_out, uint32_t width, Rows ids, float sca
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t chunks = (n + 63) / 64;
   const uint32_t fills = gridDim.x - n;
-  const bool is_fill = blockIdx.x < fills;   // (before the tokens, which wait more than they write: 4,096 of 1,024 42 us, behind 49)
+  // (the zeros before the tokens, which wait more than they write: 4,096 of 1,024 42 us, behind 49)
+  const bool is_fill = blockIdx.x < fills;
   const uint32_t number = is_fill ? blockIdx.x : blockIdx.x - fills;
   if (is_fill) {
     if (blockIdx.y) return;
@@ -231,7 +237,12 @@ few_tokens_kernel(uint32_t n, Rows grad_out, uint32_t width, Rows ids, float sca
 // Sort: least significant digit first, up to ten bits a pass and two launches: every workgroup
 // counts the digits of its part of the list, then every workgroup finds from all counts where its
 // part's tokens go.  A token's key is its number, or `vocab` (behind all others) if it has no
-// gradient.
+// gradient.  Bound by waits: of 16,384 tokens the four launches take 20 us, of 131,072 29 us.
+//
+// Sums: bound by memory.  131,072 tokens of 2,048 bf16 added to 65,536 binary32 rows (0.96 GB) take
+// 222 us without the sort, 4.3 TB/s; 16,384 tokens of 4,096 into a cleared table of 131,072 rows 55.
+// A tile is 32 tokens: with 16 more sums cross tiles (65,537 tokens, half of them one number: 113 us,
+// 107), with 64 the longest workgroups end late (131,072 tokens of 1,024 131 us, 122).
 // ---------------------------------------------------------------------------
 constexpr uint32_t kMaxBins = 1024;
 constexpr uint32_t kSortGroup = 1024, kSortWaves = kSortGroup / 64;
@@ -388,8 +399,8 @@ enum : uint32_t { kHead = 1, kWhole = 2, kGoesOn = 4 };
 
 // Zeros in those of up to 64 table rows from `v0` on that no token has: a lane looks for its row.
 template <typename Out>
-__device__ __forceinline__ void fill_rows(const TileView& s, const uint32_t* keys, uint32_t v0, uint32_t width, const Rows& grad,
-                                          uint32_t vocab) {
+__device__ __forceinline__ void fill_rows(const TileView& s, const uint32_t* keys, uint32_t v0, uint32_t width,
+                                          const Rows& grad, uint32_t vocab) {
   const uint32_t lane = threadIdx.x & 63u, v = v0 + lane;
   const bool mine = lane < s.fill_rows && v < vocab;
   uint32_t lo = 0, hi = mine ? s.n : 0u;   // the first key that is not smaller
@@ -427,8 +438,8 @@ __device__ __forceinline__ void sum_tile(const TileView& s, const uint32_t* __re
       typename Packed<In, 8>::type v[kTileStep];
 #pragma unroll
       for (uint32_t u = 0; u < kTileStep; ++u) v[u] = slice.template read<kFull>(row_at<const In>(grad_out, token[u]));
-      // (what the sums that end here are added to is asked for at the same time: one after the
-      // other, 131,072 tokens of 2,048 added to a binary32 table took 242 us)
+      // (what the sums that end here are added to is asked for at the same time: 131,072 tokens of
+      // 1,024, spread evenly, added to 131,072 bf16 rows 171 -> 162 us)
       typename Packed<Out, 8>::type held[kTileStep];
       if (accumulate) {
 #pragma unroll
@@ -479,7 +490,8 @@ tile_sum_kernel(TileView s, const uint32_t* __restrict__ keys, const uint32_t* _
   __shared__ uint32_t tile_key[32];     // a tile's first key
   __shared__ uint32_t tile_is[32];      // kHead | kWhole | kGoesOn
   const uint32_t sums = s.blocks * s.slabs, fills = gridDim.x - sums;
-  const bool is_fill = blockIdx.x >= sums;   // (behind the sums: 16,384 tokens of 4,096 244 us, before them 249, among them 266)
+  // (the zeros behind the sums: 65,537 tokens of 1,000 109 us, before them 120, among them 112)
+  const bool is_fill = blockIdx.x >= sums;
   const uint32_t number = is_fill ? blockIdx.x - sums : blockIdx.x;
   if (is_fill) {
     const uint64_t step = (uint64_t)fills * s.fill_rows;
@@ -542,7 +554,8 @@ tile_sum_kernel(TileView s, const uint32_t* __restrict__ keys, const uint32_t* _
 constexpr uint32_t kJoinWaves = 8;   // (131,072 tokens of one number: 4 wavefronts 138 us, 8 122 us)
 template <int kVec, typename Out>
 __global__ void __launch_bounds__(kJoinWaves * 64)
-tile_join_kernel(TileView s, const uint32_t* __restrict__ keys, uint32_t width, float scale, bool accumulate, Rows grad, uint32_t vocab) {
+tile_join_kernel(TileView s, const uint32_t* __restrict__ keys, uint32_t width, float scale, bool accumulate, Rows grad,
+                 uint32_t vocab) {
   __shared__ float8 share[kJoinWaves - 1][64];
   const uint32_t block = blockIdx.x, first = block * s.block, next = first + s.block;
   if (next >= s.n) return;
@@ -570,7 +583,8 @@ tile_join_kernel(TileView s, const uint32_t* __restrict__ keys, uint32_t width, 
   if (on) {
 #pragma unroll 8
     for (uint32_t p = begin; p < end; ++p)
-      sum += load<8>(s.parts + ((uint64_t)(block + p) * 2 + (p == 0 ? 1 : 0)) * s.stride + (blockIdx.y * 64u + lane) * kLaneElements);
+      sum += load<8>(s.parts + ((uint64_t)(block + p) * 2 + (p == 0 ? 1 : 0)) * s.stride +
+                     (blockIdx.y * 64u + lane) * kLaneElements);
   }
   if (wave) share[wave - 1][lane] = sum;
   __syncthreads();

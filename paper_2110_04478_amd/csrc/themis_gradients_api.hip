@@ -89,7 +89,7 @@ GradLayout grad_layout(uint32_t n, uint32_t width, uint32_t vocab) {
   l.shift = std::max(std::min(next_power(vecs), 6u), kLeastShift);
   l.slabs = (vecs + 63) / 64;
   l.stride = l.slabs * 512;
-  // Tiles: long, so that few sums cross one, as long as there is a wavefront for every SIMD four times.
+  // Tiles: 32 tokens, fewer where that leaves less than four wavefronts for every SIMD.
   l.tile = 32;
   while (l.tile > 8 && (((uint64_t)n + l.tile - 1) / l.tile * l.slabs << l.shift) / 64 < 4096) l.tile /= 2;
   l.block = l.tile * (256u >> l.shift);
@@ -120,8 +120,8 @@ void clear_table(Launches& go, const Rows& table, uint32_t width, uint32_t vocab
   const uint32_t vec = table.type == THEMIS_F32 ? 4 : 8, vecs = (width + vec - 1) / vec;
   const uint32_t shift = std::min(next_power(vecs), 8u), rows = 256u >> shift;
   with_type(table.type, [&](auto out) {
-    go(clear_rows_kernel<decltype(out)>, dim3(std::min((vocab + rows - 1) / rows, (1u << 24) - 1), std::min((vecs + 255) / 256, 65535u)), 256,
-       table, width, vocab, shift);
+    const dim3 grid(std::min((vocab + rows - 1) / rows, (1u << 24) - 1), std::min((vecs + 255) / 256, 65535u));
+    go(clear_rows_kernel<decltype(out)>, grid, 256, table, width, vocab, shift);
   });
 }
 
@@ -163,7 +163,7 @@ int themis_embedding_lookup(const themis_rows_t* table, uint64_t vocab, uint64_t
   with_type(table->type, [&](auto in) {
     with_type(out->type, [&](auto to) {
       // Four rows a lane where that leaves a workgroup for every CU four times, and past the
-      // caches (65,536 rows of 4,096: 139 us, one row 180 us; 4,096 rows of 64: 3.1 and 2.2 us).
+      // caches (65,536 rows of 4,096 139 us, with one 180; 4,096 rows of 64 3.1 and 2.2 us).
       if (n / (256u >> shift) * chunks >= 4096) run(lookup_kernel<decltype(in), decltype(to), 4>, 4);
       else run(lookup_kernel<decltype(in), decltype(to), 1>, 1);
     });
@@ -326,7 +326,7 @@ int themis_gradient_plan(const themis_gradient_t* parts, uint64_t n_parts, uint6
   plan->n_tensors = n_tensors;
   plan->n_pieces = n_pieces;
   plan->image_bytes = room;
-  plan->workspace_bytes = (pass_groups((uint32_t)n_pieces) + n_pieces) * sizeof(double);
+  plan->workspace_bytes = (pass_groups(n_pieces, bytes) + n_pieces) * sizeof(double);
   plan->in_bytes = bytes;
   plan->has_out = has_out;
   plan->strided = strided;
@@ -343,7 +343,7 @@ static int gradient_pass(const themis_gradient_plan_t* plan, double max_norm, bo
   if (!plan || !plan->image || !total || !aligned(plan->image, 16)) return THEMIS_ERR_INVALID_ARGUMENT;
   if (plan->n_pieces >= kMost || plan->n_tensors > kMostTensors) return THEMIS_ERR_UNSUPPORTED;
   if (clip && (!(max_norm > 0.0) || !std::isfinite(max_norm) || !plan->has_out)) return THEMIS_ERR_INVALID_ARGUMENT;
-  const uint32_t groups = pass_groups((uint32_t)plan->n_pieces);
+  const uint32_t groups = pass_groups(plan->n_pieces, plan->in_bytes);
   const size_t need = (groups + plan->n_pieces) * sizeof(double);
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return THEMIS_ERR_WORKSPACE;
   const PlanView view = plan_view(*plan);

@@ -512,6 +512,32 @@ def test_clip_strides(gpu):
     check_clipped(parts, before, total, check_norms(total, norms, before), 1.0)
 
 
+def test_gradients_that_share_elements(gpu):
+    """A tensor given twice, windows over one another: norms as of any other, but no scaling in place."""
+    g = normal((400,), F32, 3).cuda()
+    for grads in ([g, g], [g, g[:0], g.view(20, 20), g], [g.unfold(0, 50, 7)], [g[:5], g.unfold(0, 3, 1)]):
+        plan = gpu.themis_gradient_plan(grads)
+        total, norms = gpu.themis_gradient_norm(plan)
+        norm = check_norms(total, norms, grads)
+        if any(a is b for k, a in enumerate(grads) for b in grads[k + 1:]) or any(a.dim() == 2 and a.stride(0) < a.shape[1] for a in grads):
+            with pytest.raises(gpu.ThemisError) as e:
+                gpu.themis_gradient_clip(plan, 1.0)
+            assert e.value.status == -1
+        outs = [torch.empty(x.shape, device="cuda") for x in grads]
+        total, norms = gpu.themis_gradient_clip(gpu.themis_gradient_plan(grads, outs), 1.0)
+        check_clipped(outs, grads, total, norm, 1.0)
+    with pytest.raises(gpu.ThemisError):
+        gpu.themis_gradient_plan([g, g], [g, g])
+
+
+def test_many_tiny_gradients(gpu):
+    grads = list(normal((9000 * 3,), BF16, 4).cuda().split(3))
+    total, norms = gpu.themis_gradient_norm(gpu.themis_gradient_plan(grads))
+    want = torch.cat(grads).double().view(-1, 3).square().sum(1).cpu()
+    assert bool(((norms.double().cpu() - want.sqrt()).abs() <= 2.0 ** -23 * want.sqrt()).all())
+    assert abs(total.item() - want.sum().sqrt().item()) <= 2.0 ** -23 * total.item()
+
+
 def test_norm_needs_no_scaling(gpu):
     """Squares beyond binary32's range, in both directions, and sums of them."""
     for value in (1e-30, 1e-44, 1e25, 3e38):
