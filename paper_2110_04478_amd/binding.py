@@ -400,13 +400,13 @@ _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int32: 3,
 INVALID_ARGUMENT = -1
 
 
-def _rows(t: torch.Tensor, lead: int) -> Optional[_Rows]:
-    """t as rows of its last dimension (lead = t.dim() - 1) or of single elements (lead =
-    t.dim()), in the two levels of themis_rows; None where its strides need more."""
+def _rows(t: torch.Tensor, lead: int, width: int) -> Optional[_Rows]:
+    """t as rows of its last dimension (lead = t.dim() - 1, width elements) or of single elements
+    (lead = t.dim(), width = 1), in the two levels of themis_rows; None where its strides need
+    more."""
     if t.is_contiguous():
-        return _Rows(t.data_ptr(), _TYPES[t.dtype], t.numel() or 1, 0,
-                     t.shape[-1] if lead < t.dim() else 1)
-    if lead < t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
+        return _Rows(t.data_ptr(), _TYPES[t.dtype], 1 << 31, 0, width)   # (one level)
+    if width > 1 and t.stride(-1) != 1:
         return None
     levels = []   # (rows, stride), outermost first, merged where one stride covers both
     for n, s in zip(t.shape[:lead], t.stride()[:lead]):
@@ -423,13 +423,13 @@ def _rows(t: torch.Tensor, lead: int) -> Optional[_Rows]:
     return _Rows(t.data_ptr(), _TYPES[t.dtype], max(1, inner), outer, step)
 
 
-def _read_rows(t: torch.Tensor, lead: int) -> tuple:
+def _read_rows(t: torch.Tensor, lead: int, width: int) -> tuple:
     """(rows, the tensor that holds them): t itself, or a copy where its strides are beyond
     what the library reads."""
-    r = _rows(t, lead)
+    r = _rows(t, lead, width)
     if r is None:
         t = t.contiguous()
-        r = _rows(t, lead)
+        r = _rows(t, lead, width)
     return r, t
 
 
@@ -442,11 +442,10 @@ _FLOATS = frozenset((torch.float32, torch.bfloat16, torch.float16))
 _INDEXES = frozenset((torch.int32, torch.int64))
 
 
-def _stream_here(t: torch.Tensor) -> int:
-    """The current stream of t's GPU, which has to be the current one.  (Through the raw
+def _stream_here(device: int) -> int:
+    """The current stream of this GPU, which has to be the current one.  (Through the raw
     handle: the stream object of torch.cuda.current_stream takes 2.7 us, a quarter of a call on
     a few rows.)"""
-    device = t.get_device()
     _need(device == torch._C._cuda_getDevice())
     return torch._C._cuda_getCurrentRawStream(device)
 
@@ -456,23 +455,24 @@ def themis_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float
                             out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """scale * table[ids] -> [*ids.shape, width] of out's type (given by out or out_dtype;
     the table's otherwise).  A token number outside the table gives a row of NaN."""
-    _need(table.is_cuda and table.dim() == 2 and table.dtype in _FLOATS and ids.dtype in _INDEXES and
-          ids.get_device() == table.get_device())
+    device = table.get_device()
+    _need(device >= 0 and table.dim() == 2 and table.dtype in _FLOATS and ids.dtype in _INDEXES and
+          ids.get_device() == device)
     vocab, width = table.shape
     shape = (*ids.shape, width)
     if out is None:
         _need(out_dtype is None or out_dtype in _FLOATS)
         out = table.new_empty(shape, dtype=out_dtype)
     else:
-        _need(out.dtype in _FLOATS and out.shape == shape and out.device == table.device and
+        _need(out.dtype in _FLOATS and out.shape == shape and out.get_device() == device and
               out_dtype in (None, out.dtype))
     n = ids.numel()
     if n == 0 or width == 0:
         return out
-    stream = _stream_here(table)
-    rows_t, table = _read_rows(table, 1)
-    rows_i, ids = _read_rows(ids, ids.dim())
-    rows_o = _rows(out, out.dim() - 1)
+    stream = _stream_here(device)
+    rows_t, table = _read_rows(table, 1, width)
+    rows_i, ids = _read_rows(ids, len(shape) - 1, 1)
+    rows_o = _rows(out, len(shape) - 1, width)
     _need(rows_o is not None)
     _check(lib().themis_embedding_lookup(rows_t, vocab, width, rows_i, n, scale, rows_o, stream))
     return out
@@ -489,30 +489,34 @@ def themis_embedding_grad(grad_out: torch.Tensor, ids: torch.Tensor, vocab: int,
     """The gradient of the table behind themis_embedding_lookup -> [vocab, width] of out's type
     (given by out or out_dtype; grad_out's otherwise), or added to out where `accumulate`.
     Tokens of number `ignored`, or outside the table, have no gradient."""
-    _need(grad_out.is_cuda and grad_out.dtype in _FLOATS and ids.dtype in _INDEXES and
-          grad_out.dim() >= 1 and grad_out.shape[:-1] == ids.shape and
-          ids.get_device() == grad_out.get_device() and
+    device = grad_out.get_device()
+    shape = grad_out.shape
+    _need(device >= 0 and grad_out.dtype in _FLOATS and ids.dtype in _INDEXES and
+          len(shape) >= 1 and shape[:-1] == ids.shape and ids.get_device() == device and
           vocab >= 0 and (out is not None or not accumulate))
-    width = grad_out.shape[-1]
+    width = shape[-1]
     if out is None:
         _need(out_dtype is None or out_dtype in _FLOATS)
         out = grad_out.new_empty((vocab, width), dtype=out_dtype)
     else:
         _need(out.dtype in _FLOATS and out.shape == (vocab, width) and
-              out.device == grad_out.device and out_dtype in (None, out.dtype))
+              out.get_device() == device and out_dtype in (None, out.dtype))
     n = ids.numel()
     if vocab == 0 or width == 0 or (n == 0 and accumulate):
         return out
-    stream = _stream_here(grad_out)
-    rows_g, grad_out = _read_rows(grad_out, grad_out.dim() - 1)
-    rows_i, ids = _read_rows(ids, ids.dim())
-    rows_o = _rows(out, 1)
+    stream = _stream_here(device)
+    rows_g, grad_out = _read_rows(grad_out, len(shape) - 1, width)
+    rows_i, ids = _read_rows(ids, len(shape) - 1, 1)
+    rows_o = _rows(out, 1, width)
     _need(rows_o is not None)
     if workspace is None:
-        workspace = alloc_workspace(themis_embedding_grad_workspace_bytes(n, width, vocab), out.device)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        need = lib().themis_embedding_grad_workspace_bytes(n, width, vocab)
+        if need:
+            workspace = alloc_workspace(need, out.device)
+    at, size = (None, 0) if workspace is None else (workspace.data_ptr(),
+                                                    workspace.numel() * workspace.element_size())
     _check(lib().themis_embedding_grad(rows_g, width, rows_i, n, scale, ignored, int(accumulate),
-                                       rows_o, vocab, _ptr(workspace), ws_bytes, stream))
+                                       rows_o, vocab, at, size, stream))
     return out
 
 
@@ -606,7 +610,7 @@ def themis_gradient_norm(plan: GradientPlan):
     result = plan.image.new_empty(1 + plan.n_tensors, dtype=torch.float32)
     at = result.data_ptr()
     _check(lib().themis_gradient_norm(plan.c_struct, at, at + 4, plan.workspace_at,
-                                      plan.c_struct.workspace_bytes, _stream_here(plan.image)))
+                                      plan.c_struct.workspace_bytes, _stream_here(plan.image.get_device())))
     return result.split((1, plan.n_tensors))
 
 
@@ -616,5 +620,5 @@ def themis_gradient_clip(plan: GradientPlan, max_norm: float):
     result = plan.image.new_empty(2 + plan.n_tensors, dtype=torch.float32)
     at = result.data_ptr()
     _check(lib().themis_gradient_clip(plan.c_struct, max_norm, at, at + 8, plan.workspace_at,
-                                      plan.c_struct.workspace_bytes, _stream_here(plan.image)))
+                                      plan.c_struct.workspace_bytes, _stream_here(plan.image.get_device())))
     return result.split((2, plan.n_tensors))

@@ -80,10 +80,10 @@ GradLayout grad_layout(uint32_t n, uint32_t width, uint32_t vocab) {
   const uint32_t bits = next_power(vocab + 1);   // keys 0 .. vocab
   l.passes = (bits + 9) / 10;
   l.bits = (bits + l.passes - 1) / l.passes;
-  // A workgroup of the sort takes kSortGroup tokens in one turn, and reads the counts of all parts,
-  // eight at a time: about as long, so there are ten parts for every turn.
+  // A workgroup of the sort takes kSortGroup tokens in a turn, and reads the counts of all parts, 16 at
+  // a time: up to 40 parts for every turn (131,072 tokens: 9.6 us a move; with 20 11.4, with 80 9.7).
   l.part = kSortGroup;
-  while ((uint64_t)n > (uint64_t)l.part * (10 * (l.part / kSortGroup))) l.part *= 2;
+  while ((uint64_t)n > (uint64_t)l.part * (40 * (l.part / kSortGroup))) l.part *= 2;
   l.sort_parts = (n + l.part - 1) / l.part;
   const uint32_t vecs = (width + kLaneElements - 1) / kLaneElements;
   l.shift = std::max(std::min(next_power(vecs), 6u), kLeastShift);

@@ -221,11 +221,11 @@ def test_rows_of_tensors(binding):
     for t, lead in ((base, 2), (base, 3), (base[:, :-1], 2), (base[::2, ::3], 2), (base.transpose(0, 1), 2),
                     (base[:, 1:2], 2), (base[0, 0, 0], 0), (base[0, 0], 1), (base[0, 0], 0), (base[:, :, 3], 2),
                     (base[:1].expand(5, 6, 10), 2), (base[:, :1].expand(4, 9, 10), 2), (base[..., :7], 2)):
-        r = binding._rows(t, lead)
+        r = binding._rows(t, lead, t.shape[-1] if lead < t.dim() else 1)
         n = int(np.prod(t.shape[:lead]))
         k = np.arange(n)
         at = k // r.inner * r.outer_stride + k % r.inner * r.inner_stride
         want = (np.indices(t.shape[:lead]).reshape(lead, -1) * np.array(t.stride()[:lead]).reshape(-1, 1)).sum(0) if lead else [0]
         assert np.array_equal(at, want), (t.shape, t.stride())
-    assert binding._rows(base[..., ::2], 2) is None
-    assert binding._rows(base.permute(1, 0, 2)[::2, :, ::3], 3) is None
+    assert binding._rows(base[..., ::2], 2, 5) is None
+    assert binding._rows(base.permute(1, 0, 2)[::2, :, ::3], 3, 1) is None
