@@ -70,78 +70,85 @@ __device__ __forceinline__ void store_some(T* p, Floats<N> v, uint32_t count) {
   for (uint32_t k = 0; k < N - 1; ++k)
     if (k < count) p[k] = (T)v[k];
 }
-template <int N, typename T>
-__device__ __forceinline__ void store_some_away(T* p, Floats<N> v, uint32_t count) {
-  if (count == N) return store_away<N>(p, v);
-  store_some<N>(p, v, count);
-}
+constexpr uint32_t kLaneElements = 8;
+
+// A lane's access to elements `first`.. of a row: kVec of them.  The last access of a row is moved back
+// so that it is whole as well, and its first `skip` elements are another lane's.  Rows of less than
+// kLaneElements are read and written element by element: kWhole is false for them, and only for them.
+// (All choices are made at compile time: of two stores to one place, one of which goes past the
+// caches, the compiler makes one that does not.)
+template <int kVec>
+struct Access {
+  uint32_t at, skip, count;   // count: elements of its own (0: none)
+  __device__ __forceinline__ Access(uint32_t first, uint32_t width) {
+    count = first < width ? min(width - first, (uint32_t)kVec) : 0u;
+    // (a lane without elements of its own reads the last ones again)
+    at = width >= kLaneElements ? min(first, width - kVec) : first;
+    skip = count ? first - at : 0u;
+  }
+  template <bool kWhole, typename T>
+  __device__ __forceinline__ typename Packed<T, kVec>::type read(const T* row) const {
+    return kWhole ? load<kVec>(row + at) : load_some<kVec>(row + at, count);
+  }
+  template <bool kWhole, typename T>
+  __device__ __forceinline__ void write(T* row, Floats<kVec> v) const {
+    if (!kWhole) return store_some<kVec>(row + at, v, count);
+    if (count == kVec) return store<kVec>(row + at, v);
+    if (!count) return;
+#pragma unroll
+    for (uint32_t k = 1; k < kVec; ++k)
+      if (k >= skip) row[at + k] = (T)v[k];
+  }
+  // Where lanes that share elements, or have none of their own, write what the owner writes.
+  template <bool kWhole, bool kAway, typename T>
+  __device__ __forceinline__ void write_over(T* row, Floats<kVec> v) const {
+    if constexpr (!kWhole) {
+      store_some<kVec>(row + at, v, count);
+    } else if constexpr (kAway) {
+      store_away<kVec>(row + at, v);
+    } else {
+      store<kVec>(row + at, v);
+    }
+  }
+};
 
 // Eight elements of a row for every lane of a group of `lanes`, `first` being the group's first:
-// adjacent ones (kVec = 8), or four and four, `lanes` accesses apart (kVec = 4).  Only the last ones
-// of a row may be short of that: code that keeps loads in flight has a copy for full() lanes, whose
-// accesses are whole, and in which no load depends on a count.
+// adjacent ones (kVec = 8), or four and four, `lanes` accesses apart (kVec = 4).
 template <int kVec>
 struct Slice;
 template <>
 struct Slice<8> {
-  uint32_t at, count;
-  __device__ __forceinline__ Slice(uint32_t first, uint32_t lane, uint32_t, uint32_t width) {
-    at = first + lane * 8;
-    count = at < width ? min(width - at, 8u) : 0u;
-  }
-  __device__ __forceinline__ bool any() const { return count != 0; }
-  __device__ __forceinline__ bool full() const { return count == 8; }
-  template <bool kFull, typename T>
-  __device__ __forceinline__ typename Packed<T, 8>::type read(const T* row) const {
-    return kFull ? load<8>(row + at) : load_some<8>(row + at, count);
-  }
-  template <bool kFull, typename T>
-  __device__ __forceinline__ void write(T* row, float8 v) const {
-    if (kFull) store<8>(row + at, v);
-    else store_some<8>(row + at, v, count);
-  }
-  template <bool kFull, typename T>
-  __device__ __forceinline__ void write_away(T* row, float8 v) const {
-    if (kFull) store_away<8>(row + at, v);
-    else store_some<8>(row + at, v, count);
-  }
+  Access<8> a;
+  __device__ __forceinline__ Slice(uint32_t first, uint32_t lane, uint32_t, uint32_t width) : a(first + lane * 8, width) {}
+  __device__ __forceinline__ bool any() const { return a.count != 0; }
+  template <bool kWhole, typename T>
+  __device__ __forceinline__ typename Packed<T, 8>::type read(const T* row) const { return a.read<kWhole>(row); }
+  template <bool kWhole, typename T>
+  __device__ __forceinline__ void write(T* row, float8 v) const { a.write<kWhole>(row, v); }
+  template <bool kWhole, bool kAway, typename T>
+  __device__ __forceinline__ void write_over(T* row, float8 v) const { a.write_over<kWhole, kAway>(row, v); }
 };
 template <>
 struct Slice<4> {
-  uint32_t at, next, count, more;
-  __device__ __forceinline__ Slice(uint32_t first, uint32_t lane, uint32_t lanes, uint32_t width) {
-    at = first + lane * 4;
-    next = at + lanes * 4;
-    count = at < width ? min(width - at, 4u) : 0u;
-    more = next < width ? min(width - next, 4u) : 0u;
-    if (!more) next = at;   // (what is read there is not used)
-  }
-  __device__ __forceinline__ bool any() const { return count != 0; }
-  __device__ __forceinline__ bool full() const { return count == 4 && (more & 3u) == 0; }
-  template <bool kFull, typename T>
+  Access<4> a, b;
+  __device__ __forceinline__ Slice(uint32_t first, uint32_t lane, uint32_t lanes, uint32_t width)
+      : a(first + lane * 4, width), b(first + (lanes + lane) * 4, width) {}
+  __device__ __forceinline__ bool any() const { return a.count != 0; }
+  template <bool kWhole, typename T>
   __device__ __forceinline__ typename Packed<T, 8>::type read(const T* row) const {
-    const auto a = kFull ? load<4>(row + at) : load_some<4>(row + at, count);
-    const auto b = kFull ? load<4>(row + next) : load_some<4>(row + next, more);
-    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_shufflevector(a.read<kWhole>(row), b.read<kWhole>(row), 0, 1, 2, 3, 4, 5, 6, 7);
   }
-  template <bool kFull, typename T>
+  template <bool kWhole, typename T>
   __device__ __forceinline__ void write(T* row, float8 v) const {
-    if (kFull) {
-      store<4>(row + at, v.lo);
-      if (more) store<4>(row + next, v.hi);
-    } else {
-      store_some<4>(row + at, v.lo, count);
-      store_some<4>(row + next, v.hi, more);
-    }
+    a.write<kWhole>(row, v.lo);
+    b.write<kWhole>(row, v.hi);
   }
-  template <bool kFull, typename T>
-  __device__ __forceinline__ void write_away(T* row, float8 v) const {
-    if (!kFull) return write<false>(row, v);
-    store_away<4>(row + at, v.lo);
-    if (more) store_away<4>(row + next, v.hi);
+  template <bool kWhole, bool kAway, typename T>
+  __device__ __forceinline__ void write_over(T* row, float8 v) const {
+    a.write_over<kWhole, kAway>(row, v.lo);
+    b.write_over<kWhole, kAway>(row, v.hi);
   }
 };
-constexpr uint32_t kLaneElements = 8;
 
 __host__ __device__ constexpr bool is_float_type(int type) { return type >= THEMIS_F32 && type <= THEMIS_F16; }
 __host__ __device__ constexpr bool is_index_type(int type) { return type == THEMIS_I32 || type == THEMIS_I64; }
@@ -160,20 +167,44 @@ struct Rows {
 inline Rows rows_of(const themis_rows_t& r, uint64_t n) {
   return {(char*)r.data, r.outer_stride, r.inner_stride, r.inner < n ? (uint32_t)r.inner : 0u, r.type};
 }
+__device__ __forceinline__ int64_t row_offset(const Rows& rows, uint32_t r) {
+  if (!rows.inner) return (int64_t)r * rows.inner_stride;
+  const uint32_t outer = r / rows.inner;
+  return (int64_t)outer * rows.outer_stride + (int64_t)(r - outer * rows.inner) * rows.inner_stride;
+}
 template <typename T>
 __device__ __forceinline__ T* row_at(const Rows& rows, uint32_t r) {
-  int64_t at = (int64_t)r * rows.inner_stride;
-  if (rows.inner) {
-    const uint32_t outer = r / rows.inner;
-    at = (int64_t)outer * rows.outer_stride + (int64_t)(r - outer * rows.inner) * rows.inner_stride;
-  }
-  return (T*)rows.data + at;
+  return (T*)rows.data + row_offset(rows, r);
 }
 
-// Token number t as a table row, or ~0u for one outside the table.
+// Numbers of the tokens t[] as table rows, ~0u for those outside the table; the loads are in flight
+// together.
+template <int kTokens>
+__device__ __forceinline__ void token_rows(const Rows& ids, const uint32_t (&t)[kTokens], uint32_t vocab,
+                                           uint32_t (&row)[kTokens]) {
+  int64_t at[kTokens], id[kTokens];
+  if (!ids.inner) {
+#pragma unroll
+    for (int k = 0; k < kTokens; ++k) at[k] = (int64_t)t[k] * ids.inner_stride;
+  } else {
+#pragma unroll
+    for (int k = 0; k < kTokens; ++k) at[k] = row_offset(ids, t[k]);
+  }
+  if (ids.type == THEMIS_I64) {
+#pragma unroll
+    for (int k = 0; k < kTokens; ++k) id[k] = ((const int64_t*)ids.data)[at[k]];
+  } else {
+#pragma unroll
+    for (int k = 0; k < kTokens; ++k) id[k] = ((const int32_t*)ids.data)[at[k]];
+  }
+#pragma unroll
+  for (int k = 0; k < kTokens; ++k) row[k] = (uint64_t)id[k] < vocab ? (uint32_t)id[k] : ~0u;
+}
 __device__ __forceinline__ uint32_t token_row(const Rows& ids, uint32_t t, uint32_t vocab) {
-  const int64_t id = ids.type == THEMIS_I64 ? *row_at<const int64_t>(ids, t) : (int64_t)*row_at<const int32_t>(ids, t);
-  return (uint64_t)id < vocab ? (uint32_t)id : ~0u;
+  const uint32_t one[1] = {t};
+  uint32_t row[1];
+  token_rows(ids, one, vocab, row);
+  return row[0];
 }
 
 // Calls f with a value of the element type that `type` names.

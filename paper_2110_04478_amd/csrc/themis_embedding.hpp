@@ -15,17 +15,18 @@ namespace themis {
 // once) in 133 us, 5.3 TB/s, where a copy of 4 GiB makes 4.8 and one of 128 MiB 7.2; a few rows take
 // the time of a launch.
 // ---------------------------------------------------------------------------
-template <bool kFull, int kRows, typename In, typename Out, int kVec>
+template <bool kWhole, int kRows, typename In, typename Out, int kVec>
 __device__ __forceinline__ void lookup_rows(const Slice<kVec>& slice, const Rows& table, uint32_t vocab, const Rows& ids,
                                             uint32_t n, float scale, const Rows& out, uint32_t t0, uint32_t groups) {
-  uint32_t row[kRows];
+  uint32_t token[kRows], row[kRows];
 #pragma unroll
-  for (int k = 0; k < kRows; ++k) row[k] = token_row(ids, min(t0 + k * groups, n - 1u), vocab);
+  for (int k = 0; k < kRows; ++k) token[k] = min(t0 + k * groups, n - 1u);
+  token_rows(ids, token, vocab, row);
   typename Packed<In, 8>::type v[kRows];
   if (vocab) {
 #pragma unroll
     for (int k = 0; k < kRows; ++k)   // (row 0 in the place of none: its values are not used)
-      v[k] = slice.template read<kFull>(row_at<const In>(table, row[k] == ~0u ? 0u : row[k]));
+      v[k] = slice.template read<kWhole>(row_at<const In>(table, row[k] == ~0u ? 0u : row[k]));
   }
 #pragma unroll
   for (int k = 0; k < kRows; ++k) {
@@ -33,12 +34,11 @@ __device__ __forceinline__ void lookup_rows(const Slice<kVec>& slice, const Rows
     if (t >= n) break;
     const float8 nan = __builtin_nanf("");
     const float8 x = row[k] != ~0u ? widen<8>(v[k]) * scale : nan;
-    if (kRows > 1) slice.template write_away<kFull>(row_at<Out>(out, t), x);
-    else slice.template write<kFull>(row_at<Out>(out, t), x);
+    slice.template write_over<kWhole, (kRows > 1)>(row_at<Out>(out, t), x);
   }
 }
 
-template <typename In, typename Out, int kRows>
+template <bool kWhole, typename In, typename Out, int kRows>
 __global__ void __launch_bounds__(256)
 lookup_kernel(Rows table, uint32_t vocab, uint32_t width, Rows ids, uint32_t n, float scale, Rows out, uint32_t shift) {
   const uint32_t lanes = 1u << shift;
@@ -48,8 +48,7 @@ lookup_kernel(Rows table, uint32_t vocab, uint32_t width, Rows ids, uint32_t n, 
   const uint32_t step = groups * kRows;
   for (uint64_t first = (uint64_t)blockIdx.x * step; first < n; first += (uint64_t)gridDim.x * step) {
     const uint32_t t0 = (uint32_t)first + (threadIdx.x >> shift);   // (below 2^32: n is below 2^31)
-    if (slice.full()) lookup_rows<true, kRows, In, Out>(slice, table, vocab, ids, n, scale, out, t0, groups);
-    else lookup_rows<false, kRows, In, Out>(slice, table, vocab, ids, n, scale, out, t0, groups);
+    lookup_rows<kWhole, kRows, In, Out>(slice, table, vocab, ids, n, scale, out, t0, groups);
   }
 }
 
@@ -69,7 +68,7 @@ constexpr uint32_t kRowsInFlight = 8;
 constexpr uint32_t kMostGroups = 32;
 constexpr uint32_t kScan = 4;   // token numbers of a lane in flight
 
-template <bool kFull, typename In, int kVec>
+template <bool kWhole, typename In, int kVec>
 __device__ __forceinline__ float8 sum_listed(const Slice<kVec>& slice, const Rows& grad_out, const uint16_t* list,
                                              uint32_t begin, uint32_t end) {
   float8 sum = 0.0f;
@@ -78,19 +77,19 @@ __device__ __forceinline__ float8 sum_listed(const Slice<kVec>& slice, const Row
     typename Packed<In, 8>::type v[kRowsInFlight];
 #pragma unroll
     for (uint32_t u = 0; u < kRowsInFlight; ++u)
-      v[u] = slice.template read<kFull>(row_at<const In>(grad_out, list[i + u]));
+      v[u] = slice.template read<kWhole>(row_at<const In>(grad_out, list[i + u]));
 #pragma unroll
     for (uint32_t u = 0; u < kRowsInFlight; ++u) sum += widen<8>(v[u]);
   }
 #pragma unroll 2
-  for (; i < end; ++i) sum += widen<8>(slice.template read<kFull>(row_at<const In>(grad_out, list[i])));
+  for (; i < end; ++i) sum += widen<8>(slice.template read<kWhole>(row_at<const In>(grad_out, list[i])));
   return sum;
 }
 
 // Zeros in the rows of `empty` behind v0, by a workgroup: short rows side by side.  kAway: past the
 // caches (beside sums that need them: 65,537 tokens of 1,000 108 us, through them 116; alone it is
 // 200 MB in 52 us and 45).
-template <bool kAway, typename Out>
+template <bool kWhole, bool kAway, typename Out>
 __device__ __forceinline__ void write_zeros(uint64_t empty, uint32_t v0, uint32_t width, const Rows& grad) {
   constexpr int kVec = kVecOf<Out>;
   const uint32_t vecs = (width + kVec - 1) / kVec;
@@ -98,11 +97,8 @@ __device__ __forceinline__ void write_zeros(uint64_t empty, uint32_t v0, uint32_
   for (uint32_t r = threadIdx.x >> shift; r < 64; r += 256u >> shift) {
     if (!((empty >> r) & 1u)) continue;
     Out* to = row_at<Out>(grad, v0 + r);
-    for (uint32_t c = threadIdx.x & ((1u << shift) - 1u); c < vecs; c += 256) {
-      const uint32_t count = min(width - c * kVec, (uint32_t)kVec);
-      if (kAway) store_some_away<kVec>(to + c * kVec, Floats<kVec>(0.0f), count);
-      else store_some<kVec>(to + c * kVec, Floats<kVec>(0.0f), count);
-    }
+    for (uint32_t c = threadIdx.x & ((1u << shift) - 1u); c < vecs; c += 256)
+      Access<kVec>(c * kVec, width).template write_over<kWhole, kAway>(to, Floats<kVec>(0.0f));
   }
 }
 
@@ -120,28 +116,28 @@ __global__ void __launch_bounds__(256) clear_kernel(char* table, uint64_t bytes)
   if (rest < bytes) table[rest] = 0;
 }
 // The same, rows that do not follow each other: 2^shift lanes a row, or 4 KiB of one.
-template <typename Out>
+template <bool kWhole, typename Out>
 __global__ void __launch_bounds__(256)
 clear_rows_kernel(Rows table, uint32_t width, uint32_t vocab, uint32_t shift) {
-  constexpr uint32_t kVec = kVecOf<Out>;
+  constexpr int kVec = kVecOf<Out>;
   for (uint64_t c = ((uint64_t)blockIdx.y * 256u + (threadIdx.x & ((1u << shift) - 1u))) * kVec; c < width;
        c += (uint64_t)gridDim.y * 256u * kVec)
     for (uint64_t v = (uint64_t)blockIdx.x * (256u >> shift) + (threadIdx.x >> shift); v < vocab;
          v += (uint64_t)gridDim.x * (256u >> shift))
-      store_some<kVec>(row_at<Out>(table, (uint32_t)v) + c, Floats<kVec>(0.0f), min(width - (uint32_t)c, kVec));
+      Access<kVec>((uint32_t)c, width).template write_over<kWhole, false>(row_at<Out>(table, (uint32_t)v), Floats<kVec>(0.0f));
 }
 
-template <bool kFull, int kVec, typename Out>
+template <bool kWhole, int kVec, typename Out>
 __device__ __forceinline__ void write_sum(const Rows& grad, uint32_t v, const Slice<kVec>& slice, float8 sum, float scale,
                                           bool accumulate) {
   Out* to = row_at<Out>(grad, v);
   float8 x = sum * scale;
-  if (accumulate) x = widen<8>(slice.template read<kFull>((const Out*)to)) + x;
-  slice.template write<kFull>(to, x);
+  if (accumulate) x = widen<8>(slice.template read<kWhole>((const Out*)to)) + x;
+  slice.template write<kWhole>(to, x);
 }
 
 // The last n workgroups: the tokens; the others write the zeros of up to 64 rows at a time.
-template <typename In, typename Out>
+template <bool kWhole, typename In, typename Out>
 __global__ void __launch_bounds__(256)
 few_tokens_kernel(uint32_t n, Rows grad_out, uint32_t width, Rows ids, float scale, uint32_t ignored, bool accumulate,
                   Rows grad, uint32_t vocab, uint32_t fill_rows) {
@@ -162,23 +158,31 @@ few_tokens_kernel(uint32_t n, Rows grad_out, uint32_t width, Rows ids, float sca
       __syncthreads();
       if (threadIdx.x == 0) masks[0] = 0;
       __syncthreads();
-#pragma unroll 4
-      for (uint32_t t = threadIdx.x; t < n; t += 256) {
-        const uint32_t id = token_row(ids, t, vocab), at = id - v0;
-        if (id >= v0 && at < rows && id != ignored) atomicOr((unsigned long long*)&masks[0], 1ull << at);
+      for (uint32_t t = threadIdx.x; t < n; t += 256 * kScan) {
+        uint32_t token[kScan], found[kScan];
+#pragma unroll
+        for (uint32_t k = 0; k < kScan; ++k) token[k] = min(t + k * 256, n - 1u);
+        token_rows(ids, token, vocab, found);
+#pragma unroll
+        for (uint32_t k = 0; k < kScan; ++k) {
+          const uint32_t at = found[k] - v0;
+          if (t + k * 256 < n && found[k] >= v0 && at < rows && found[k] != ignored)
+            atomicOr((unsigned long long*)&masks[0], 1ull << at);
+        }
       }
       __syncthreads();
       const uint64_t all = rows == 64 ? ~0ull : (1ull << rows) - 1;
-      write_zeros<false, Out>(all & ~masks[0], v0, width, grad);
+      write_zeros<kWhole, false, Out>(all & ~masks[0], v0, width, grad);
     }
     return;
   }
   const uint32_t t = number, id = token_row(ids, t, vocab);
   if (id == ~0u || id == ignored) return;
   for (uint32_t c = wave * kScan; c < chunks; c += 4 * kScan) {
-    uint32_t found[kScan];
+    uint32_t at[kScan], found[kScan];
 #pragma unroll
-    for (uint32_t k = 0; k < kScan; ++k) found[k] = token_row(ids, min((c + k) * 64 + lane, n - 1u), vocab);
+    for (uint32_t k = 0; k < kScan; ++k) at[k] = min((c + k) * 64 + lane, n - 1u);
+    token_rows(ids, at, vocab, found);
 #pragma unroll
     for (uint32_t k = 0; k < kScan; ++k) {
       const uint64_t mine = __ballot((c + k) * 64 + lane < n && found[k] == id);
@@ -214,15 +218,14 @@ few_tokens_kernel(uint32_t n, Rows grad_out, uint32_t width, Rows ids, float sca
     constexpr int kVec = kVecOf<In>;
     const Slice<kVec> slice(k * lanes * kLaneElements, threadIdx.x & (lanes - 1u), lanes, width);
     float8 sum = 0.0f;
-    if (slice.full()) sum = sum_listed<true, In>(slice, grad_out, list, begin, end);
-    else if (slice.any()) sum = sum_listed<false, In>(slice, grad_out, list, begin, end);
+    if (slice.any()) sum = sum_listed<kWhole, In>(slice, grad_out, list, begin, end);
     if (groups > 1) {
       part[threadIdx.x] = sum;
       __syncthreads();
       if (group == 0)
         for (uint32_t g = 1; g < groups; ++g) sum += part[(g << shift) + threadIdx.x];
     }
-    if (group == 0 && slice.any()) write_sum<false, kVec, Out>(grad, id, slice, sum, scale, accumulate);
+    if (group == 0 && slice.any()) write_sum<kWhole, kVec, Out>(grad, id, slice, sum, scale, accumulate);
     if (groups > 1) __syncthreads();
   }
 }
@@ -260,11 +263,18 @@ struct SortView {
   uint32_t* token_out;
 };
 
-__device__ __forceinline__ uint32_t sort_key(const SortView& s, const Rows& ids, uint32_t vocab, uint32_t ignored,
-                                             uint32_t i) {
-  if (s.key_in) return s.key_in[i];
-  const uint32_t id = token_row(ids, i, vocab);
-  return id == ~0u || id == ignored ? vocab : id;
+// Keys of the places i[] of the list.
+template <int kKeys>
+__device__ __forceinline__ void sort_keys(const SortView& s, const Rows& ids, uint32_t vocab, uint32_t ignored,
+                                          const uint32_t (&i)[kKeys], uint32_t (&key)[kKeys]) {
+  if (s.key_in) {
+#pragma unroll
+    for (int k = 0; k < kKeys; ++k) key[k] = s.key_in[i[k]];
+    return;
+  }
+  token_rows(ids, i, vocab, key);
+#pragma unroll
+  for (int k = 0; k < kKeys; ++k) key[k] = key[k] == ~0u || key[k] == ignored ? vocab : key[k];
 }
 
 // One more of `digit` in `bins`, for every lane that is on.  (Lanes with the first lane's digit go
@@ -286,9 +296,10 @@ sort_count_kernel(SortView s, Rows ids, uint32_t vocab, uint32_t ignored) {
   for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) count[b] = 0;
   __syncthreads();
   for (uint32_t i = first + threadIdx.x; i - lane < last; i += kSortAhead * kSortGroup) {
-    uint32_t key[kSortAhead];
+    uint32_t at[kSortAhead], key[kSortAhead];
 #pragma unroll
-    for (uint32_t k = 0; k < kSortAhead; ++k) key[k] = sort_key(s, ids, vocab, ignored, min(i + k * kSortGroup, last - 1u));
+    for (uint32_t k = 0; k < kSortAhead; ++k) at[k] = min(i + k * kSortGroup, last - 1u);
+    sort_keys(s, ids, vocab, ignored, at, key);
 #pragma unroll
     for (uint32_t k = 0; k < kSortAhead; ++k) {
       if (i - lane + k * kSortGroup >= last) break;   // (the wavefront's first)
@@ -313,9 +324,10 @@ sort_move_kernel(SortView s, Rows ids, uint32_t vocab, uint32_t ignored) {
     for (uint32_t w = 0; w < kSortWaves; ++w) place[w][b] = 0;
   __syncthreads();
   for (uint32_t i = begin; i < end; i += kSortAhead * 64) {
-    uint32_t key[kSortAhead];
+    uint32_t at[kSortAhead], key[kSortAhead];
 #pragma unroll
-    for (uint32_t k = 0; k < kSortAhead; ++k) key[k] = sort_key(s, ids, vocab, ignored, min(i + k * 64 + lane, end - 1u));
+    for (uint32_t k = 0; k < kSortAhead; ++k) at[k] = min(i + k * 64 + lane, end - 1u);
+    sort_keys(s, ids, vocab, ignored, at, key);
 #pragma unroll
     for (uint32_t k = 0; k < kSortAhead; ++k) {
       if (i + k * 64 >= end) break;
@@ -356,13 +368,12 @@ sort_move_kernel(SortView s, Rows ids, uint32_t vocab, uint32_t ignored) {
     }
   __syncthreads();
   for (uint32_t i0 = begin; i0 < end; i0 += kSortAhead * 64) {
-    uint32_t keys[kSortAhead], tokens[kSortAhead];
+    uint32_t from[kSortAhead], keys[kSortAhead], tokens[kSortAhead];
 #pragma unroll
-    for (uint32_t k = 0; k < kSortAhead; ++k) {
-      const uint32_t i = min(i0 + k * 64 + lane, end - 1u);
-      keys[k] = sort_key(s, ids, vocab, ignored, i);
-      tokens[k] = s.key_in ? s.token_in[i] : i;
-    }
+    for (uint32_t k = 0; k < kSortAhead; ++k) from[k] = min(i0 + k * 64 + lane, end - 1u);
+    sort_keys(s, ids, vocab, ignored, from, keys);
+#pragma unroll
+    for (uint32_t k = 0; k < kSortAhead; ++k) tokens[k] = s.key_in ? s.token_in[from[k]] : from[k];
 #pragma unroll
     for (uint32_t k = 0; k < kSortAhead; ++k) {
       if (i0 + k * 64 >= end) break;
@@ -400,10 +411,10 @@ struct TileView {
 };
 constexpr uint32_t kTileStep = 8;    // rows in flight
 constexpr uint32_t kLeastShift = 3;  // (up to 32 groups of lanes)
-enum : uint32_t { kHead = 1, kWhole = 2, kGoesOn = 4 };
+enum : uint32_t { kHead = 1, kOneSum = 2, kGoesOn = 4 };
 
 // Zeros in those of up to 64 table rows from `v0` on that no token has: a lane looks for its row.
-template <typename Out>
+template <bool kWhole, typename Out>
 __device__ __forceinline__ void fill_rows(const TileView& s, const uint32_t* keys, uint32_t v0, uint32_t width,
                                           const Rows& grad, uint32_t vocab) {
   const uint32_t lane = threadIdx.x & 63u, v = v0 + lane;
@@ -416,12 +427,12 @@ __device__ __forceinline__ void fill_rows(const TileView& s, const uint32_t* key
       else hi = mid;
     }
   }
-  write_zeros<true, Out>(__ballot(mine && (lo >= s.n || keys[lo] != v)), v0, width, grad);
+  write_zeros<kWhole, true, Out>(__ballot(mine && (lo >= s.n || keys[lo] != v)), v0, width, grad);
 }
 
 // A tile's sums: those that begin and end in it to the table, the others to `head` (one that began
 // before) and `tail`.
-template <bool kFull, typename In, typename Out, int kVec>
+template <bool kWhole, typename In, typename Out, int kVec>
 __device__ __forceinline__ void sum_tile(const TileView& s, const uint32_t* __restrict__ keys,
                                          const uint32_t* __restrict__ tokens, const Slice<kVec>& slice,
                                          const Rows& grad_out, float scale, bool accumulate, const Rows& grad,
@@ -442,14 +453,14 @@ __device__ __forceinline__ void sum_tile(const TileView& s, const uint32_t* __re
     if (some == kTileStep && key[kTileStep - 1] < vocab) {
       typename Packed<In, 8>::type v[kTileStep];
 #pragma unroll
-      for (uint32_t u = 0; u < kTileStep; ++u) v[u] = slice.template read<kFull>(row_at<const In>(grad_out, token[u]));
+      for (uint32_t u = 0; u < kTileStep; ++u) v[u] = slice.template read<kWhole>(row_at<const In>(grad_out, token[u]));
       // (what the sums that end here are added to is asked for at the same time: 131,072 tokens of
       // 1,024, spread evenly, added to 131,072 bf16 rows 171 -> 162 us)
       typename Packed<Out, 8>::type held[kTileStep];
       if (accumulate) {
 #pragma unroll
         for (uint32_t u = 0; u < kTileStep; ++u)
-          if (key[u + 1] != key[u]) held[u] = slice.template read<kFull>(row_at<const Out>(grad, key[u]));
+          if (key[u + 1] != key[u]) held[u] = slice.template read<kWhole>(row_at<const Out>(grad, key[u]));
       }
 #pragma unroll
       for (uint32_t u = 0; u < kTileStep; ++u) {
@@ -463,7 +474,7 @@ __device__ __forceinline__ void sum_tile(const TileView& s, const uint32_t* __re
         } else {
           float8 x = sum * scale;
           if (accumulate) x = widen<8>(held[u]) + x;
-          slice.template write<kFull>(row_at<Out>(grad, key[u]), x);
+          slice.template write<kWhole>(row_at<Out>(grad, key[u]), x);
         }
         before = false;
         sum = 0.0f;
@@ -472,12 +483,12 @@ __device__ __forceinline__ void sum_tile(const TileView& s, const uint32_t* __re
       for (uint32_t u = 0; u < some; ++u) {
         const uint32_t k = keys[j + u];
         if (k >= vocab) return;
-        sum += widen<8>(slice.template read<kFull>(row_at<const In>(grad_out, tokens[j + u])));
+        sum += widen<8>(slice.template read<kWhole>(row_at<const In>(grad_out, tokens[j + u])));
         const bool goes_on = j + u + 1 < s.n && keys[j + u + 1] == k;
         if (goes_on && j + u + 1 < last) continue;
         if (before) head = sum;
         else if (goes_on) tail = sum;
-        else write_sum<kFull, kVec, Out>(grad, k, slice, sum, scale, accumulate);
+        else write_sum<kWhole, kVec, Out>(grad, k, slice, sum, scale, accumulate);
         before = false;
         sum = 0.0f;
       }
@@ -486,14 +497,14 @@ __device__ __forceinline__ void sum_tile(const TileView& s, const uint32_t* __re
 }
 
 // kWave: a wavefront for every tile, all of whose lanes go the same way.
-template <typename In, typename Out, bool kWave>
+template <bool kWhole, typename In, typename Out, bool kWave>
 __global__ void __launch_bounds__(256)
 tile_sum_kernel(TileView s, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ tokens, Rows grad_out,
                 uint32_t width, float scale, bool accumulate, Rows grad, uint32_t vocab) {
   // A group's sums that its tile does not hold whole: of one that began before, of one that goes on.
   __shared__ float8 part[2][256];
   __shared__ uint32_t tile_key[32];     // a tile's first key
-  __shared__ uint32_t tile_is[32];      // kHead | kWhole | kGoesOn
+  __shared__ uint32_t tile_is[32];      // kHead | kOneSum | kGoesOn
   const uint32_t sums = s.blocks * s.slabs, fills = gridDim.x - sums;
   // (the zeros behind the sums: 65,537 tokens of 1,000 109 us, before them 120, among them 112)
   const bool is_fill = blockIdx.x >= sums;
@@ -501,7 +512,7 @@ tile_sum_kernel(TileView s, const uint32_t* __restrict__ keys, const uint32_t* _
   if (is_fill) {
     const uint64_t step = (uint64_t)fills * s.fill_rows;
     for (uint64_t v = (uint64_t)number * s.fill_rows; v < vocab; v += step)
-      fill_rows<Out>(s, keys, (uint32_t)v, width, grad, vocab);
+      fill_rows<kWhole, Out>(s, keys, (uint32_t)v, width, grad, vocab);
     return;
   }
   const uint32_t shift = kWave ? 6u : s.shift, lanes = 1u << shift;
@@ -513,16 +524,13 @@ tile_sum_kernel(TileView s, const uint32_t* __restrict__ keys, const uint32_t* _
   const uint32_t first = block * s.block + group * s.tile, last = min(first + s.tile, s.n);
   if (slice.any() && first < last) {
     float8 head = 0.0f, tail = 0.0f;
-    if (slice.full())
-      sum_tile<true, In, Out>(s, keys, tokens, slice, grad_out, scale, accumulate, grad, vocab, first, last, head, tail);
-    else
-      sum_tile<false, In, Out>(s, keys, tokens, slice, grad_out, scale, accumulate, grad, vocab, first, last, head, tail);
+    sum_tile<kWhole, In, Out>(s, keys, tokens, slice, grad_out, scale, accumulate, grad, vocab, first, last, head, tail);
     part[0][threadIdx.x] = head;
     part[1][threadIdx.x] = tail;
     if ((threadIdx.x & (lanes - 1u)) == 0) {
       const uint32_t k0 = keys[first], k1 = keys[last - 1];
       tile_key[group] = k0;
-      tile_is[group] = (first > 0 && keys[first - 1] == k0 ? kHead : 0u) | (k0 == k1 ? kWhole : 0u) |
+      tile_is[group] = (first > 0 && keys[first - 1] == k0 ? kHead : 0u) | (k0 == k1 ? kOneSum : 0u) |
                        (k1 < vocab && last < s.n && keys[last] == k1 ? kGoesOn : 0u);
     }
   }
@@ -531,12 +539,12 @@ tile_sum_kernel(TileView s, const uint32_t* __restrict__ keys, const uint32_t* _
   // What crosses tiles is put together by the group in whose tile it ends; what crosses the block's
   // ends is left to tile_join_kernel.
   const uint32_t is = tile_is[group], own = threadIdx.x & (lanes - 1u);
-  const bool ends = (is & kHead) && (is & (kWhole | kGoesOn)) != (kWhole | kGoesOn);
+  const bool ends = (is & kHead) && (is & (kOneSum | kGoesOn)) != (kOneSum | kGoesOn);
   const bool leaves = (is & kGoesOn) && last == block_end;
   if (tile_key[group] >= vocab || !(ends || leaves)) return;
   uint32_t from = group;   // the tile it begins in, or the block's first
   bool before = is & kHead;
-  while (before && from > 0) before = (tile_is[--from] & (kHead | kWhole)) == (kHead | kWhole);
+  while (before && from > 0) before = (tile_is[--from] & (kHead | kOneSum)) == (kHead | kOneSum);
   float8 sum = 0.0f;
   if (is & kHead) {
     sum = part[before ? 0 : 1][(from << shift) + own];
@@ -545,7 +553,7 @@ tile_sum_kernel(TileView s, const uint32_t* __restrict__ keys, const uint32_t* _
   float* out = s.parts + (uint64_t)block * 2 * s.stride + (slab * 64u + own) * kLaneElements;
   if (ends) {
     if (before) store<8>(out, sum);
-    else write_sum<false, kVec, Out>(grad, tile_key[group], slice, sum, scale, accumulate);
+    else write_sum<kWhole, kVec, Out>(grad, tile_key[group], slice, sum, scale, accumulate);
   }
   if (leaves) {
     const bool own_tail = !(is & kHead) || ends;   // it began in this tile
@@ -557,7 +565,7 @@ tile_sum_kernel(TileView s, const uint32_t* __restrict__ keys, const uint32_t* _
 // Adds the parts of a sum that crosses blocks: a workgroup for every block in which one begins and
 // does not end, its wavefronts a share of the parts each, in order.
 constexpr uint32_t kJoinWaves = 8;   // (131,072 tokens of one number: 4 wavefronts 138 us, 8 122 us)
-template <int kVec, typename Out>
+template <bool kWhole, int kVec, typename Out>
 __global__ void __launch_bounds__(kJoinWaves * 64)
 tile_join_kernel(TileView s, const uint32_t* __restrict__ keys, uint32_t width, float scale, bool accumulate, Rows grad,
                  uint32_t vocab) {
@@ -596,7 +604,7 @@ tile_join_kernel(TileView s, const uint32_t* __restrict__ keys, uint32_t width, 
   if (wave || !on) return;
 #pragma unroll
   for (uint32_t w = 0; w < kJoinWaves - 1; ++w) sum += share[w][lane];
-  write_sum<false, kVec, Out>(grad, v, slice, sum, scale, accumulate);
+  write_sum<kWhole, kVec, Out>(grad, v, slice, sum, scale, accumulate);
 }
 
 }  // namespace themis

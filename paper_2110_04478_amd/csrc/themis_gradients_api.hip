@@ -121,7 +121,7 @@ void clear_table(Launches& go, const Rows& table, uint32_t width, uint32_t vocab
   const uint32_t shift = std::min(next_power(vecs), 8u), rows = 256u >> shift;
   with_type(table.type, [&](auto out) {
     const dim3 grid(std::min((vocab + rows - 1) / rows, (1u << 24) - 1), std::min((vecs + 255) / 256, 65535u));
-    go(clear_rows_kernel<decltype(out)>, grid, 256, table, width, vocab, shift);
+    go(width < kLaneElements ? clear_rows_kernel<false, decltype(out)> : clear_rows_kernel<true, decltype(out)>, grid, 256, table, width, vocab, shift);
   });
 }
 
@@ -162,10 +162,13 @@ int themis_embedding_lookup(const themis_rows_t* table, uint64_t vocab, uint64_t
   };
   with_type(table->type, [&](auto in) {
     with_type(out->type, [&](auto to) {
-      // Four rows a lane where that leaves a workgroup for every CU four times, and past the
-      // caches (65,536 rows of 4,096 139 us, with one 180; 4,096 rows of 64 3.1 and 2.2 us).
-      if (n / (256u >> shift) * chunks >= 4096) run(lookup_kernel<decltype(in), decltype(to), 4>, 4);
-      else run(lookup_kernel<decltype(in), decltype(to), 1>, 1);
+      // Two rows a lane, written past the caches, where workgroups of one row would be sixteen for
+      // every CU (65,536 rows of 4,096: with one 180 us, two 133, three 137, four 145).
+      typedef decltype(in) In;
+      typedef decltype(to) Out;
+      if (width < kLaneElements) run(lookup_kernel<false, In, Out, 1>, 1);
+      else if (n / (256u >> shift) * chunks >= 4096) run(lookup_kernel<true, In, Out, 2>, 2);
+      else run(lookup_kernel<true, In, Out, 1>, 1);
     });
   });
   return go.status();
@@ -201,7 +204,9 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
     const uint32_t columns = (uint32_t)std::min<uint64_t>((width + 2047) / 2048, std::max<uint64_t>(1, 1024 / std::max<uint64_t>(n, 1)));
     with_type(g.type, [&](auto in) {
       with_type(to.type, [&](auto out) {
-        go(few_tokens_kernel<decltype(in), decltype(out)>, dim3((uint32_t)(n + fill), columns), 256, (uint32_t)n, g,
+        typedef decltype(in) In;
+        typedef decltype(out) Out;
+        go(width < kLaneElements ? few_tokens_kernel<false, In, Out> : few_tokens_kernel<true, In, Out>, dim3((uint32_t)(n + fill), columns), 256, (uint32_t)n, g,
            (uint32_t)width, k, scale, skip, accumulate != 0, to, (uint32_t)vocab, fill_rows);
       });
     });
@@ -240,10 +245,13 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
     with_type(to.type, [&](auto out) {
       typedef decltype(in) In;
       typedef decltype(out) Out;
-      go(l.shift == 6 ? tile_sum_kernel<In, Out, true> : tile_sum_kernel<In, Out, false>, dim3((uint32_t)(sums + fill)),
-         256, t, keys, tokens, g, (uint32_t)width, scale, accumulate != 0, to, (uint32_t)vocab);
+      go(width < kLaneElements ? tile_sum_kernel<false, In, Out, false>
+         : l.shift < 6         ? tile_sum_kernel<true, In, Out, false>
+                               : tile_sum_kernel<true, In, Out, true>,
+         dim3((uint32_t)(sums + fill)), 256, t, keys, tokens, g, (uint32_t)width, scale, accumulate != 0, to, (uint32_t)vocab);
       if (l.blocks > 1)
-        go(tile_join_kernel<kVecOf<In, Out>, Out>, dim3(l.blocks - 1, l.slabs), kJoinWaves * 64, t, keys, (uint32_t)width, scale,
+        go(width < kLaneElements ? tile_join_kernel<false, kVecOf<In, Out>, Out> : tile_join_kernel<true, kVecOf<In, Out>, Out>,
+           dim3(l.blocks - 1, l.slabs), kJoinWaves * 64, t, keys, (uint32_t)width, scale,
            accumulate != 0, to, (uint32_t)vocab);
     });
   });

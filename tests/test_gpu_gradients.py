@@ -337,6 +337,45 @@ def test_grad_against_differences(gpu):
         assert abs(value(moved) - value(table) - want) <= (n + 4) * U * size
 
 
+@pytest.mark.parametrize("kinds", [(F32, F32), (BF16, BF16), (F16, F32), (F32, BF16)])
+@pytest.mark.parametrize("width", [2, 3, 4, 5, 7, 9, 11, 15, 17, 259, 511, 513, 515, 1023, 2047, 2049, 2051, 4099])
+def test_rows_that_end_inside_an_access(gpu, width, kinds):
+    """Every element is written once, and nothing beside the row: the last access of a row is moved
+    back over the one before."""
+    kind, to = kinds
+    for n in (40, 4500):
+        vocab = 70
+        table, ids = normal((vocab, width), kind, n), numbers(n, vocab, I64, width)
+        wide = torch.full((n, width + 5), 7.0, dtype=to, device="cuda")
+        gpu.themis_embedding_lookup(table.cuda(), ids.cuda(), 1.7, out=wide[:, 2:-3])
+        same(wide[:, 2:-3], lookup_64(table, ids, 1.7, to))
+        g, held = normal((n, width), kind, 1), normal((vocab, width), to, 2)
+        for add in (False, True):
+            whole = torch.full((vocab, width + 5), 7.0, dtype=to, device="cuda")
+            whole[:, 3:-2] = held.cuda()
+            gpu.themis_embedding_grad(g.cuda(), ids.cuda(), vocab, 1.3, out=whole[:, 3:-2], accumulate=add)
+            check_grad(whole[:, 3:-2], g, ids, vocab, 1.3, held=held if add else None)
+            whole[:, 3:-2] = 7.0
+            assert bool((whole == 7.0).all())
+        wide[:, 2:-3] = 7.0
+        assert bool((wide == 7.0).all())
+
+
+@pytest.mark.parametrize("pad", [0, 1, 4, 8])
+@pytest.mark.parametrize("width", [40, 1001, 2400])
+def test_large_tables_cleared_before_the_sums(gpu, width, pad):
+    """Tables beyond 64 MiB: rows that follow each other, and rows that do not; at odd addresses."""
+    vocab = (80 << 20) // (4 * width)
+    whole = torch.full((vocab * (width + pad) + 3,), 7.0, device="cuda")
+    out = torch.as_strided(whole, (vocab, width), (width + pad, 1), 1)
+    n = 50
+    g, ids = normal((n, width), F32, 1), torch.randint(0, vocab, (n,), generator=torch.Generator().manual_seed(5))
+    gpu.themis_embedding_grad(g.cuda(), ids.cuda(), vocab, 2.0, out=out)
+    check_grad(out, g, ids, vocab, 2.0)
+    out.fill_(7.0)
+    assert bool((whole == 7.0).all())
+
+
 @pytest.mark.parametrize("n", [4095, 4096, 4097, 4160, 8192, 9001])
 @pytest.mark.parametrize("width", [1, 9, 64, 65, 300, 777, 1032])
 def test_grad_on_both_sides_of_the_sort(gpu, n, width):
