@@ -563,22 +563,26 @@ tile_sum_kernel(TileView s, const uint32_t* __restrict__ keys, const uint32_t* _
 }
 
 // Adds the parts of a sum that crosses blocks: a workgroup for every block in which one begins and
-// does not end, its wavefronts a share of the parts each, in order.
-constexpr uint32_t kJoinWaves = 8;   // (131,072 tokens of one number: 4 wavefronts 138 us, 8 122 us)
-template <bool kWhole, int kVec, typename Out>
-__global__ void __launch_bounds__(kJoinWaves * 64)
+// does not end, its wavefronts a share of the parts each, in order.  (Eight wavefronts, which wait for
+// few parts each where one token has many; four where there are so many workgroups that these end one
+// after the other: 65,537 tokens, half of them one number, 102 us with eight and 105 with four; the
+// joins of 131,072 tokens of 4,096 37 us and 24.)
+template <bool kWhole, int kVec, typename Out, int kWaves>
+__global__ void __launch_bounds__(kWaves * 64)
 tile_join_kernel(TileView s, const uint32_t* __restrict__ keys, uint32_t width, float scale, bool accumulate, Rows grad,
                  uint32_t vocab) {
-  __shared__ float8 share[kJoinWaves - 1][64];
+  __shared__ float8 share[kWaves - 1][64];
   const uint32_t block = blockIdx.x, first = block * s.block, next = first + s.block;
   if (next >= s.n) return;
-  const uint32_t v = keys[next - 1];
-  if (v >= vocab || keys[next] != v) return;
-  if (first > 0 && keys[first - 1] == v) return;   // it began before
+  const uint32_t after = min(next + s.block, s.n - 1u);   // (the block behind the next begins here, if there is one)
+  const uint32_t v = keys[next - 1], v_next = keys[next], v_after = keys[after], v_before = keys[first > 0 ? first - 1 : 0];
+  if (v >= vocab || v_next != v) return;
+  if (first > 0 && v_before == v) return;   // it began before
   const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
-  // The blocks behind this one that it reaches into: those whose first key is v.  Every lane looks
-  // at one of 64 places, which are nearer to each other each time.
+  // The blocks behind this one that it reaches into, those whose first key is v: mostly one.  Where
+  // there are more every lane looks at one of 64 places, which are nearer to each other each time.
   uint32_t lo = block + 1, hi = s.blocks;   // block lo is one, block hi (if there is one) is none
+  if (v_after != v) hi = lo + 1;
   while (hi - lo > 1) {
     const uint32_t step = (hi - lo + 63) / 64;
     const uint64_t at = (uint64_t)lo + (uint64_t)lane * step;
@@ -591,7 +595,7 @@ tile_join_kernel(TileView s, const uint32_t* __restrict__ keys, uint32_t width, 
   const uint32_t terms = lo - block + 1;
   const Slice<kVec> slice(blockIdx.y * 512u, lane & ((1u << s.shift) - 1u), 1u << s.shift, width);
   const bool on = lane >> s.shift == 0 && slice.any();
-  const uint32_t each = (terms + kJoinWaves - 1) / kJoinWaves, begin = min(wave * each, terms), end = min(begin + each, terms);
+  const uint32_t each = (terms + kWaves - 1) / kWaves, begin = min(wave * each, terms), end = min(begin + each, terms);
   float8 sum = 0.0f;
   if (on) {
 #pragma unroll 8
@@ -603,7 +607,7 @@ tile_join_kernel(TileView s, const uint32_t* __restrict__ keys, uint32_t width, 
   __syncthreads();
   if (wave || !on) return;
 #pragma unroll
-  for (uint32_t w = 0; w < kJoinWaves - 1; ++w) sum += share[w][lane];
+  for (uint32_t w = 0; w < kWaves - 1; ++w) sum += share[w][lane];
   write_sum<kWhole, kVec, Out>(grad, v, slice, sum, scale, accumulate);
 }
 

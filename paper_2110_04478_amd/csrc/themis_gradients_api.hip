@@ -249,10 +249,15 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
          : l.shift < 6         ? tile_sum_kernel<true, In, Out, false>
                                : tile_sum_kernel<true, In, Out, true>,
          dim3((uint32_t)(sums + fill)), 256, t, keys, tokens, g, (uint32_t)width, scale, accumulate != 0, to, (uint32_t)vocab);
-      if (l.blocks > 1)
-        go(width < kLaneElements ? tile_join_kernel<false, kVecOf<In, Out>, Out> : tile_join_kernel<true, kVecOf<In, Out>, Out>,
-           dim3(l.blocks - 1, l.slabs), kJoinWaves * 64, t, keys, (uint32_t)width, scale,
-           accumulate != 0, to, (uint32_t)vocab);
+      constexpr int kVec = kVecOf<In, Out>;
+      auto join = [&](auto kernel, unsigned waves) {
+        go(kernel, dim3(l.blocks - 1, l.slabs), waves * 64, t, keys, (uint32_t)width, scale, accumulate != 0, to,
+           (uint32_t)vocab);
+      };
+      if (l.blocks < 2) return;
+      if (width < kLaneElements) join(tile_join_kernel<false, kVec, Out, 8>, 8);
+      else if (sums <= 2048) join(tile_join_kernel<true, kVec, Out, 8>, 8);
+      else join(tile_join_kernel<true, kVec, Out, 4>, 4);
     });
   });
   return go.status();
