@@ -157,8 +157,15 @@ __device__ __forceinline__ void tensor_norms(const PlanView& plan, uint32_t bloc
                                              const double* __restrict__ piece_sums, float* __restrict__ norms) {
   const uint32_t t = block * 4u + (threadIdx.x >> 6);
   if (t >= plan.n_tensors) return;
+  const uint32_t end = plan.first[t + 1];
   double x = 0.0;
-  for (uint32_t i = plan.first[t] + (threadIdx.x & 63u); i < plan.first[t + 1]; i += 64) x += piece_sums[i];
+  for (uint32_t i = plan.first[t] + (threadIdx.x & 63u); i < end; i += 64 * kInFlight) {
+    double s[kInFlight];
+#pragma unroll
+    for (uint32_t k = 0; k < kInFlight; ++k) s[k] = piece_sums[min(i + k * 64, end - 1u)];
+#pragma unroll
+    for (uint32_t k = 0; k < kInFlight; ++k) x += i + k * 64 < end ? s[k] : 0.0;
+  }
   x = wave_sum(x);
   if ((threadIdx.x & 63u) == 0) norms[t] = (float)sqrt(x);
 }
