@@ -47,8 +47,8 @@ class _Gradient(C.Structure):
 
 class _GradientPlan(C.Structure):
     _fields_ = [("n_tensors", C.c_uint64), ("n_pieces", C.c_uint64), ("image_bytes", C.c_uint64),
-                ("workspace_bytes", C.c_uint64), ("in_bytes", C.c_uint64), ("has_out", C.c_uint32), ("strided", C.c_uint32),
-                ("image", _vp)]
+                ("workspace_bytes", C.c_uint64), ("in_bytes", C.c_uint64), ("has_out", C.c_uint32),
+                ("strided", C.c_uint32), ("image", _vp)]
 
 
 _lib = None
@@ -611,7 +611,7 @@ def themis_gradient_norm(plan: GradientPlan):
     at = result.data_ptr()
     _check(lib().themis_gradient_norm(plan.c_struct, at, at + 4, plan.workspace_at,
                                       plan.c_struct.workspace_bytes, _stream_here(plan.image.get_device())))
-    return result.split((1, plan.n_tensors))
+    return torch.split_with_sizes(result, (1, plan.n_tensors))
 
 
 def themis_gradient_clip(plan: GradientPlan, max_norm: float):
@@ -621,4 +621,4 @@ def themis_gradient_clip(plan: GradientPlan, max_norm: float):
     at = result.data_ptr()
     _check(lib().themis_gradient_clip(plan.c_struct, max_norm, at, at + 8, plan.workspace_at,
                                       plan.c_struct.workspace_bytes, _stream_here(plan.image.get_device())))
-    return result.split((2, plan.n_tensors))
+    return torch.split_with_sizes(result, (2, plan.n_tensors))

@@ -124,7 +124,8 @@ clear_rows_kernel(Rows table, uint32_t width, uint32_t vocab, uint32_t shift) {
        c += (uint64_t)gridDim.y * 256u * kVec)
     for (uint64_t v = (uint64_t)blockIdx.x * (256u >> shift) + (threadIdx.x >> shift); v < vocab;
          v += (uint64_t)gridDim.x * (256u >> shift))
-      Access<kVec>((uint32_t)c, width).template write_over<kWhole, false>(row_at<Out>(table, (uint32_t)v), Floats<kVec>(0.0f));
+      Access<kVec>((uint32_t)c, width)
+          .template write_over<kWhole, false>(row_at<Out>(table, (uint32_t)v), Floats<kVec>(0.0f));
 }
 
 template <bool kWhole, int kVec, typename Out>
@@ -387,9 +388,10 @@ sort_move_kernel(SortView s, Rows ids, uint32_t vocab, uint32_t ignored) {
       const uint32_t rank = (uint32_t)__popcll(same & ((1ull << lane) - 1));
       // (all lanes have read before the first of a digit's adds: a wavefront's accesses to LDS are
       // served in the order of the program, and these are kept in it)
-      const uint32_t to = (on ? __hip_atomic_load(&place[wave][digit], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0u) + rank;
+      uint32_t* next = &place[wave][digit];
+      const uint32_t to = (on ? __hip_atomic_load(next, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0u) + rank;
       if (on && rank == 0)
-        __hip_atomic_store(&place[wave][digit], to + (uint32_t)__popcll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        __hip_atomic_store(next, to + (uint32_t)__popcll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
       if (on) {
         s.key_out[to] = keys[k];
         s.token_out[to] = tokens[k];

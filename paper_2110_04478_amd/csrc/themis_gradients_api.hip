@@ -121,7 +121,9 @@ void clear_table(Launches& go, const Rows& table, uint32_t width, uint32_t vocab
   const uint32_t shift = std::min(next_power(vecs), 8u), rows = 256u >> shift;
   with_type(table.type, [&](auto out) {
     const dim3 grid(std::min((vocab + rows - 1) / rows, (1u << 24) - 1), std::min((vecs + 255) / 256, 65535u));
-    go(width < kLaneElements ? clear_rows_kernel<false, decltype(out)> : clear_rows_kernel<true, decltype(out)>, grid, 256, table, width, vocab, shift);
+    typedef decltype(out) Out;
+    go(width < kLaneElements ? clear_rows_kernel<false, Out> : clear_rows_kernel<true, Out>, grid, 256, table, width,
+       vocab, shift);
   });
 }
 
@@ -195,19 +197,22 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
   const uint32_t skip = ignored >= 0 && (uint64_t)ignored < vocab ? (uint32_t)ignored : ~0u;
   Launches go(stream);
   // (a workgroup's zeros: about 256 KiB, in up to 64 rows)
-  const uint32_t fill_rows = (uint32_t)std::min<uint64_t>(64, std::max<uint64_t>(1, (256u << 10) / (width * type_bytes(to.type))));
+  const uint64_t row_bytes = width * type_bytes(to.type);
+  const uint32_t fill_rows = (uint32_t)std::min<uint64_t>(64, std::max<uint64_t>(1, (256u << 10) / row_bytes));
   const bool clear = !accumulate && clears(n, vocab, width, to.type);
   const uint64_t fill = accumulate || clear ? 0 : std::min<uint64_t>((vocab + fill_rows - 1) / fill_rows, 1u << 20);
   if (clear) clear_table(go, to, (uint32_t)width, (uint32_t)vocab);
   if (n == 0) return go.status();
   if (n <= kFewTokens) {
-    const uint32_t columns = (uint32_t)std::min<uint64_t>((width + 2047) / 2048, std::max<uint64_t>(1, 1024 / std::max<uint64_t>(n, 1)));
+    // (a row that one token has is 2,048 elements for a workgroup, of longer ones several while there are few)
+    const uint32_t columns = (uint32_t)std::min<uint64_t>((width + 2047) / 2048, n < 1024 ? 1024 / n : 1);
     with_type(g.type, [&](auto in) {
       with_type(to.type, [&](auto out) {
         typedef decltype(in) In;
         typedef decltype(out) Out;
-        go(width < kLaneElements ? few_tokens_kernel<false, In, Out> : few_tokens_kernel<true, In, Out>, dim3((uint32_t)(n + fill), columns), 256, (uint32_t)n, g,
-           (uint32_t)width, k, scale, skip, accumulate != 0, to, (uint32_t)vocab, fill_rows);
+        go(width < kLaneElements ? few_tokens_kernel<false, In, Out> : few_tokens_kernel<true, In, Out>,
+           dim3((uint32_t)(n + fill), columns), 256, (uint32_t)n, g, (uint32_t)width, k, scale, skip, accumulate != 0, to,
+           (uint32_t)vocab, fill_rows);
       });
     });
     return go.status();
@@ -248,7 +253,8 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
       go(width < kLaneElements ? tile_sum_kernel<false, In, Out, false>
          : l.shift < 6         ? tile_sum_kernel<true, In, Out, false>
                                : tile_sum_kernel<true, In, Out, true>,
-         dim3((uint32_t)(sums + fill)), 256, t, keys, tokens, g, (uint32_t)width, scale, accumulate != 0, to, (uint32_t)vocab);
+         dim3((uint32_t)(sums + fill)), 256, t, keys, tokens, g, (uint32_t)width, scale, accumulate != 0, to,
+         (uint32_t)vocab);
       constexpr int kVec = kVecOf<In, Out>;
       auto join = [&](auto kernel, unsigned waves) {
         go(kernel, dim3(l.blocks - 1, l.slabs), waves * 64, t, keys, (uint32_t)width, scale, accumulate != 0, to,
