@@ -493,7 +493,8 @@ def themis_embedding_grad(grad_out: torch.Tensor, ids: torch.Tensor, vocab: int,
     shape = grad_out.shape
     _need(device >= 0 and grad_out.dtype in _FLOATS and ids.dtype in _INDEXES and
           len(shape) >= 1 and shape[:-1] == ids.shape and ids.get_device() == device and
-          vocab >= 0 and (out is not None or not accumulate))
+          vocab >= 0 and (out is not None or not accumulate) and
+          (workspace is None or (workspace.get_device() == device and workspace.is_contiguous())))
     width = shape[-1]
     if out is None:
         _need(out_dtype is None or out_dtype in _FLOATS)

@@ -87,3 +87,17 @@ def test_a_training_iteration(gradients):
     # (binary32 products over up to 376 tokens and 256 elements: far within 1e-3)
     assert abs(got["losses"][0] - loss.item()) < 1e-3 * loss.item()
     assert abs(got["norms"][0] - norm) < 1e-3 * norm
+
+
+@pytest.mark.parametrize("n", [3, 5000])
+def test_workspaces_elsewhere_are_refused(gradients, n):
+    """Host memory, and memory with gaps or of one element that a stride of zero makes long."""
+    binding = gradients.binding
+    ids = torch.zeros(n, dtype=torch.int64, device="cuda")
+    g = torch.zeros((n, 8), device="cuda")
+    need = 2 * max(16, binding.themis_embedding_grad_workspace_bytes(n, 8, 5))
+    for work in (torch.empty(need, dtype=torch.uint8), torch.empty(need, dtype=torch.uint8, device="cuda")[::2],
+                 torch.empty(1, dtype=torch.uint8, device="cuda").expand(need)):
+        with pytest.raises(binding.ThemisError) as e:
+            binding.themis_embedding_grad(g, ids, 5, workspace=work)
+        assert e.value.status == -1
