@@ -7,6 +7,7 @@ from typing import Optional
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding
 
@@ -19,6 +20,7 @@ class _Embedding(torch.autograd.Function):
         return binding.themis_embedding_lookup(table, ids, scale)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_out):
         (ids,) = ctx.saved_tensors
         vocab, dtype, scale, ignored, into = ctx.args
@@ -35,7 +37,7 @@ def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, ignore
 
     into: where the gradient is added in place of being returned to autograd (table.grad, say: a
     table that is also the output projection has one already, and only the rows of the tokens at
-    hand are touched)."""
+    hand are touched).  Differentiable once: a derivative through the gradient raises an error."""
     return _Embedding.apply(table, ids, float(scale), int(ignored), into)
 
 

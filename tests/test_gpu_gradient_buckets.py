@@ -101,3 +101,14 @@ def test_workspaces_elsewhere_are_refused(gradients, n):
         with pytest.raises(binding.ThemisError) as e:
             binding.themis_embedding_grad(g, ids, 5, workspace=work)
         assert e.value.status == -1
+
+
+def test_embedding_is_differentiable_once(gradients):
+    """A second derivative is an error, not a graph that ends without one."""
+    table = torch.ones((5, 8), device="cuda", requires_grad=True)
+    ids = torch.tensor([1, 4, 1], device="cuda")
+    out = gradients.embedding(table, ids)
+    (grad,) = torch.autograd.grad(out.square().sum(), table, create_graph=True)
+    assert torch.equal(grad.detach()[:, 0].cpu(), torch.tensor([0.0, 4.0, 0.0, 0.0, 2.0]))
+    with pytest.raises(RuntimeError):
+        grad.sum().backward()
