@@ -564,6 +564,33 @@ def _views(g: torch.Tensor, o: Optional[torch.Tensor]):
         yield x, y, rows, cols, ra, ca, rb, cb
 
 
+def _targets_share(grads: list, outs: list) -> bool:
+    """Whether some target is given twice, or overlaps another target or a gradient that is not
+    its own in place.  (Tensors of adjacent elements, and equal views; other views with gaps may
+    lie between one another and are the caller's to know.)"""
+    places = [(o.data_ptr(), o.shape, o.stride()) for o in outs if o.numel()]
+    if len(places) != len(set(places)):
+        return True
+    spans = []   # (begin, end, written)
+    for g, o in zip(grads, outs):
+        at = o.data_ptr()
+        if o.is_contiguous():
+            spans.append((at, at + o.numel() * o.element_size(), True))
+        if g is not o and g.is_contiguous() and not (g.data_ptr() == at and g.dtype == o.dtype and o.is_contiguous()):
+            spans.append((g.data_ptr(), g.data_ptr() + g.numel() * g.element_size(), False))
+    read = written = 0   # the ends of what came before
+    for begin, end, out in sorted(spans):
+        if begin == end:
+            continue
+        if begin < written or (out and begin < read):
+            return True
+        if out:
+            written = max(written, end)
+        else:
+            read = max(read, end)
+    return False
+
+
 def themis_gradient_plan(grads, out=None) -> GradientPlan:
     """Lays out a list of gradients for themis_gradient_norm and themis_gradient_clip.
 
@@ -578,8 +605,7 @@ def themis_gradient_plan(grads, out=None) -> GradientPlan:
           all(o.dtype in _FLOATS and o.shape == g.shape and o.device == g.device for g, o in zip(grads, outs)))
     # (gradients that are their own targets and share elements, a broadcast or one given twice,
     # cannot be scaled in place: then only norms are to be had)
-    places = [(o.data_ptr(), tuple(o.shape), o.stride()) for o in outs if o.numel()]
-    twice = len(places) != len(set(places))
+    twice = _targets_share(grads, outs)
     _need(out is None or not twice)
     plan = _GradientPlan()
     for with_out in ((False,) if twice else (True, False) if out is None else (True,)):

@@ -744,3 +744,23 @@ def test_refusals(gpu):
         with pytest.raises(gpu.ThemisError) as e:
             call()
         assert e.value.status == -1, k
+
+
+def test_gradients_that_overlap_in_part(gpu):
+    """Windows over one another would be scaled twice in place, and a target on another gradient
+    before that is read: the first have norms alone, the second are refused."""
+    x, y = normal((400,), F32, 3).cuda(), normal((400,), F32, 4).cuda()
+    before = x.clone()
+    plan = gpu.themis_gradient_plan([x[:201], x[200:]])
+    check_norms(*gpu.themis_gradient_norm(plan), [x[:201], x[200:]])
+    with pytest.raises(gpu.ThemisError) as e:
+        gpu.themis_gradient_clip(plan, 1e-3)
+    assert e.value.status == -1
+    same(x, before)
+    for grads, outs in (([x, y], [y, x]), ([x[:200]], [x[1:201]]), ([x, y], [torch.empty_like(x), x])):
+        with pytest.raises(gpu.ThemisError) as e:
+            gpu.themis_gradient_plan(grads, outs)
+        assert e.value.status == -1
+    halves = [x[:200], x[200:]]
+    total, norms = gpu.themis_gradient_clip(gpu.themis_gradient_plan(halves), 1.0)
+    check_clipped(halves, [before[:200], before[200:]], total, check_norms(total, norms, [before[:200], before[200:]]), 1.0)

@@ -229,3 +229,20 @@ def test_rows_of_tensors(binding):
         assert np.array_equal(at, want), (t.shape, t.stride())
     assert binding._rows(base[..., ::2], 2, 5) is None
     assert binding._rows(base.permute(1, 0, 2)[::2, :, ::3], 3, 1) is None
+
+
+def test_targets_that_share_memory(binding):
+    """Windows over one another, and targets on what another gradient still has to be read from."""
+    import torch
+    x, y, z = torch.zeros(40), torch.zeros(40), torch.zeros(40, dtype=torch.bfloat16)
+    share = binding._targets_share
+    for grads, outs in (([x, y], [x, y]), ([x, y], [y.clone(), x.clone()]), ([x, x], [y[:20], y[20:]]), ([], []),
+                        ([x[:20], x[20:]], [x[:20], x[20:]]), ([x[:20], x[20:]], [x[:20], y[20:]]),
+                        ([x[::2], x[1::2]], [x[::2], x[1::2]]), ([x[5:5], x], [x[5:5], x]), ([x, y[:0]], [x, x[3:3]]),
+                        ([x.view(5, 8), y], [x.view(8, 5).view(5, 8), y])):
+        assert not share(grads, outs)
+    for grads, outs in (([x, x], [x, x]), ([x[:21], x[20:]], [x[:21], x[20:]]), ([x, x[20:]], [x, x[20:]]),
+                        ([x[:10], x, x[30:]], [x[:10], x, x[30:]]), ([x, y], [y, x]), ([x, y], [x.clone(), x]),
+                        ([x[:20]], [x[1:21]]), ([z[:20], x], [x.view(torch.bfloat16)[:20], y]),
+                        ([x[::2], y[:20]], [x[::2], x[::2]])):
+        assert share(grads, outs)
