@@ -532,10 +532,21 @@ class GradientPlan:
     workspace: Optional[torch.Tensor]
     c_struct: _GradientPlan
     n_tensors: int
+    streams: set   # raw handles: the one it was made on, and others that have used it
 
     @property
     def device(self):
         return self.image.device
+
+    def stream(self) -> int:
+        """The current stream; the plan's memory, once it is given up, waits for it."""
+        stream = _stream_here(self.image.get_device())
+        if stream not in self.streams:
+            self.streams.add(stream)
+            for t in (self.image, self.workspace):
+                if t is not None:
+                    t.record_stream(torch.cuda.current_stream())
+        return stream
 
     @property
     def workspace_at(self) -> Optional[int]:
@@ -626,10 +637,11 @@ def themis_gradient_plan(grads, out=None) -> GradientPlan:
     _check(lib().themis_gradient_plan(array, len(parts), len(grads), plan, image.ctypes.data,
                                       image.nbytes))
     device = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
+    streams = {torch._C._cuda_getCurrentRawStream(device.index)}
     on_device = torch.from_numpy(image.view(np.int64)).to(device)
     plan.image = on_device.data_ptr()
     return GradientPlan(grads, None if out is None else outs, on_device,
-                        alloc_workspace(plan.workspace_bytes, device), plan, len(grads))
+                        alloc_workspace(plan.workspace_bytes, device), plan, len(grads), streams)
 
 
 def themis_gradient_norm(plan: GradientPlan):
@@ -637,7 +649,7 @@ def themis_gradient_norm(plan: GradientPlan):
     result = plan.image.new_empty(1 + plan.n_tensors, dtype=torch.float32)
     at = result.data_ptr()
     _check(lib().themis_gradient_norm(plan.c_struct, at, at + 4, plan.workspace_at,
-                                      plan.c_struct.workspace_bytes, _stream_here(plan.image.get_device())))
+                                      plan.c_struct.workspace_bytes, plan.stream()))
     return torch.split_with_sizes(result, (1, plan.n_tensors))
 
 
@@ -647,5 +659,5 @@ def themis_gradient_clip(plan: GradientPlan, max_norm: float):
     result = plan.image.new_empty(2 + plan.n_tensors, dtype=torch.float32)
     at = result.data_ptr()
     _check(lib().themis_gradient_clip(plan.c_struct, max_norm, at, at + 8, plan.workspace_at,
-                                      plan.c_struct.workspace_bytes, _stream_here(plan.image.get_device())))
+                                      plan.c_struct.workspace_bytes, plan.stream()))
     return torch.split_with_sizes(result, (2, plan.n_tensors))

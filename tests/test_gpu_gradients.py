@@ -764,3 +764,26 @@ def test_gradients_that_overlap_in_part(gpu):
     halves = [x[:200], x[200:]]
     total, norms = gpu.themis_gradient_clip(gpu.themis_gradient_plan(halves), 1.0)
     check_clipped(halves, [before[:200], before[200:]], total, check_norms(total, norms, [before[:200], before[200:]]), 1.0)
+
+
+def test_plans_given_up_while_another_stream_uses_them(gpu):
+    """The memory of a plan is not handed out again before a call on another stream has ended."""
+    grads = [normal((70001,), F32, 5).cuda()]
+    outs = [torch.empty_like(grads[0])]
+    slow = torch.ones((8192, 8192), dtype=BF16, device="cuda")
+    plan = gpu.themis_gradient_plan(grads, outs)
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        for _ in range(40):
+            slow @ slow
+        total, norms = gpu.themis_gradient_clip(plan, 1.0)
+        done = torch.cuda.Event()
+        done.record()
+    sizes, held = (plan.image.numel() * 8, plan.workspace.numel()), {plan.image.data_ptr(), plan.workspace.data_ptr()}
+    del plan
+    taken = [torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(8)]
+    if not done.query():
+        assert not held & {t.data_ptr() for t in taken}
+    other.synchronize()
+    check_clipped(outs, grads, total, check_norms(total, norms, grads), 1.0)
