@@ -524,7 +524,7 @@ typedef struct themis_rows {
  *   ids   : n token numbers, THEMIS_I32 / _I64
  *   out   : n rows of `width`, any of the three types; rows must not overlap
  *           each other nor the inputs.
- * vocab, n and width below 2^31, else THEMIS_ERR_UNSUPPORTED.
+ * vocab and n below 2^31, width up to 2^26, else THEMIS_ERR_UNSUPPORTED.
  */
 int themis_embedding_lookup(const themis_rows_t *table, uint64_t vocab, uint64_t width,
                             const themis_rows_t *ids, uint64_t n, float scale,
@@ -548,7 +548,8 @@ int themis_embedding_lookup(const themis_rows_t *table, uint64_t vocab, uint64_t
  *   workspace : themis_embedding_grad_workspace_bytes(n, width, vocab) bytes,
  *               16-byte aligned, untouched until the stream has drained, one
  *               per call in flight.
- * vocab, n and width below 2^31, else THEMIS_ERR_UNSUPPORTED.
+ * vocab, n and width below 2^31, beyond 4,096 tokens width up to 2^24 and n times
+ * width up to 2^38, else THEMIS_ERR_UNSUPPORTED.
  */
 size_t themis_embedding_grad_workspace_bytes(uint64_t n, uint64_t width, uint64_t vocab);
 int themis_embedding_grad(const themis_rows_t *grad_out, uint64_t width,
