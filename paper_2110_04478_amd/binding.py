@@ -14,6 +14,8 @@ from typing import Optional
 import numpy as np
 import torch
 
+from . import overlap
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libthemis_hip.so")
 
@@ -576,38 +578,29 @@ def _views(g: torch.Tensor, o: Optional[torch.Tensor]):
 
 
 def _targets_share(grads: list, outs: list) -> bool:
-    """Whether some target is given twice, or overlaps another target or a gradient that is not
-    its own in place.  (Tensors of adjacent elements, and equal views; other views with gaps may
-    lie between one another and are the caller's to know.)"""
-    places = [(o.data_ptr(), o.shape, o.stride()) for o in outs if o.numel()]
-    if len(places) != len(set(places)):
-        return True
-    spans = []   # (begin, end, written)
+    """Whether some element of a target is given twice, or is one of a gradient that is not this
+    target's own in place."""
+    targets, others = [], []
     for g, o in zip(grads, outs):
-        at = o.data_ptr()
-        if o.is_contiguous():
-            spans.append((at, at + o.numel() * o.element_size(), True))
-        if g is not o and g.is_contiguous() and not (g.data_ptr() == at and g.dtype == o.dtype and o.is_contiguous()):
-            spans.append((g.data_ptr(), g.data_ptr() + g.numel() * g.element_size(), False))
-    read = written = 0   # the ends of what came before
-    for begin, end, out in sorted(spans):
-        if begin == end:
+        if o.numel() == 0:
             continue
-        if begin < written or (out and begin < read):
+        if overlap.repeats(o):
             return True
-        if out:
-            written = max(written, end)
-        else:
-            read = max(read, end)
-    return False
+        place = overlap.view_of(o)
+        targets.append(place)
+        if g is not o and (g.dtype != o.dtype or overlap.view_of(g) != place):
+            others.append(overlap.view_of(g))
+    return overlap.shared(targets, others)
 
 
 def themis_gradient_plan(grads, out=None) -> GradientPlan:
     """Lays out a list of gradients for themis_gradient_norm and themis_gradient_clip.
 
     out: where the clipped gradients go, tensors of the gradients' shapes and any of the three
-    types (parts of a flat bucket, say); the gradients themselves where it is not given.  Good
-    for as long as the tensors stay where they are; their values may change."""
+    types (parts of a flat bucket, say); the gradients themselves where it is not given.  Targets
+    that share an element with each other, or with a gradient that is not theirs, are refused;
+    gradients that share elements and have no other targets have norms alone.  Good for as long
+    as the tensors stay where they are; their values may change."""
     grads = list(grads)
     _need(all(g.dtype in _FLOATS and g.is_cuda for g in grads) and
           len({g.device for g in grads}) <= 1)
