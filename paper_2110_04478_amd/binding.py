@@ -7,6 +7,7 @@ library has not been built (python paper_2110_04478_amd/csrc/build.py).
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -444,6 +445,15 @@ _FLOATS = frozenset((torch.float32, torch.bfloat16, torch.float16))
 _INDEXES = frozenset((torch.int32, torch.int64))
 
 
+# (0.3 us; what a call writes shares no memory with what it reads where their storages differ, and is
+# looked at by _apart where not)
+_one_storage = torch._C._is_alias_of
+
+
+def _apart(out: torch.Tensor, *inputs) -> bool:
+    return not overlap.shared([overlap.view_of(out)], [overlap.view_of(t) for t in inputs if t.numel()])
+
+
 def _stream_here(device: int) -> int:
     """The current stream of this GPU, which has to be the current one.  (Through the raw
     handle: the stream object of torch.cuda.current_stream takes 2.7 us, a quarter of a call on
@@ -462,7 +472,8 @@ def themis_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float
           ids.get_device() == device)
     vocab, width = table.shape
     shape = (*ids.shape, width)
-    if out is None:
+    given = out is not None
+    if not given:
         _need(out_dtype is None or out_dtype in _FLOATS)
         out = table.new_empty(shape, dtype=out_dtype)
     else:
@@ -476,10 +487,13 @@ def themis_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float
     rows_i, ids = _read_rows(ids, len(shape) - 1, 1)
     rows_o = _rows(out, len(shape) - 1, width)
     _need(rows_o is not None)
+    if given and (_one_storage(out, table) or _one_storage(out, ids)):
+        _need(_apart(out, table, ids))
     _check(lib().themis_embedding_lookup(rows_t, vocab, width, rows_i, n, scale, rows_o, stream))
     return out
 
 
+@functools.lru_cache(maxsize=1024)   # (a function of the sizes alone; a call of the library takes 0.6 us)
 def themis_embedding_grad_workspace_bytes(n: int, width: int, vocab: int) -> int:
     return lib().themis_embedding_grad_workspace_bytes(n, width, vocab)
 
@@ -498,7 +512,8 @@ def themis_embedding_grad(grad_out: torch.Tensor, ids: torch.Tensor, vocab: int,
           vocab >= 0 and (out is not None or not accumulate) and
           (workspace is None or (workspace.get_device() == device and workspace.is_contiguous())))
     width = shape[-1]
-    if out is None:
+    given = out is not None
+    if not given:
         _need(out_dtype is None or out_dtype in _FLOATS)
         out = grad_out.new_empty((vocab, width), dtype=out_dtype)
     else:
@@ -512,8 +527,10 @@ def themis_embedding_grad(grad_out: torch.Tensor, ids: torch.Tensor, vocab: int,
     rows_i, ids = _read_rows(ids, len(shape) - 1, 1)
     rows_o = _rows(out, 1, width)
     _need(rows_o is not None)
+    if given and (_one_storage(out, grad_out) or _one_storage(out, ids)):
+        _need(_apart(out, grad_out, ids))
     if workspace is None:
-        need = lib().themis_embedding_grad_workspace_bytes(n, width, vocab)
+        need = themis_embedding_grad_workspace_bytes(n, width, vocab)
         if need:
             workspace = alloc_workspace(need, out.device)
     at, size = (None, 0) if workspace is None else (workspace.data_ptr(),

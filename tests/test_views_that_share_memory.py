@@ -79,3 +79,12 @@ def test_a_search_that_is_too_long(monkeypatch):
     assert overlap.shared(odd, [])
     few = [(k, [(s, 1) for s in steps[:3]], 1) for k in (0, 5 * 10 ** 6 + 1)]
     assert not overlap.shared(few, [])
+
+
+def test_results_on_what_is_read():
+    big, ids = torch.zeros(40, 20), torch.zeros(9, dtype=torch.int64)
+    apart = binding._apart
+    assert apart(big[:9, :8], big[:, 8:16], ids) and apart(big[:9], big[9:], ids) and apart(big[::2, :4], big[1::2, :4])
+    assert apart(big[:9, :8], big[:0, :8], ids) and apart(big, big.clone(), ids)
+    assert not apart(big[:9], big, ids) and not apart(big[:9, :8], big[8:, 7:15], ids)
+    assert not apart(big[20:29, :8], big[:, :8], ids) and not apart(ids.view(torch.float32)[None], big, ids)
