@@ -44,8 +44,9 @@ def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, ignore
 class GradientBuckets:
     """The gradients of a list of parameters, and the flat buckets that carry them.
 
-    Every parameter gets a .grad of zeros that stays where it is (use zero(), not
-    zero_grad(set_to_none=True)); the buckets are filled in the order in which gradients become
+    Every parameter gets a .grad of zeros that has to stay: zero_grad(set_to_none=True), a backward
+    with create_graph and moves of the module put others in its place, and clip() is an error until
+    zero() has put these back (after moves of the module: new buckets).  The buckets are filled in the order in which gradients become
     ready, the last parameter's first, each with at least bucket_bytes unless it is the last."""
 
     def __init__(self, params, bucket_bytes: int, dtype: torch.dtype = torch.bfloat16):
@@ -69,13 +70,20 @@ class GradientBuckets:
         self.plan = binding.themis_gradient_plan([p.grad for p in self.params],
                                                  [self.views[p] for p in self.params])
 
+        self.places = [g.data_ptr() for g in self.plan.grads]
+
+    def _stays(self) -> bool:
+        return all(g.data_ptr() == at for g, at in zip(self.plan.grads, self.places))
+
     def zero(self):
-        for p in self.params:
-            p.grad.zero_()
+        binding._need(self._stays())
+        for p, g in zip(self.params, self.plan.grads):
+            p.grad = g.zero_()
 
     def clip(self, max_norm: float):
         """The clipped gradients into the buckets -> (f32[2]: norm and factor, norms of the
         parameters' gradients f32[n])."""
+        binding._need(self._stays() and all(p.grad is g for p, g in zip(self.params, self.plan.grads)))
         return binding.themis_gradient_clip(self.plan, max_norm)
 
     def sizes(self) -> np.ndarray:
