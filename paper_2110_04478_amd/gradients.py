@@ -3,6 +3,7 @@ token table whose gradient the library sums, and the flat buckets that an
 iteration's collectives carry."""
 from __future__ import annotations
 
+import contextlib
 from typing import Optional
 
 import numpy as np
@@ -12,23 +13,68 @@ from torch.autograd.function import once_differentiable
 from . import binding
 
 
+@contextlib.contextmanager
+def _behind(stream, *tensors):
+    """The current stream of the tensors' GPU waits for what has been put on `stream`."""
+    with torch.cuda.device(tensors[0].device):
+        here = torch.cuda.current_stream()
+        if here != stream:
+            here.wait_stream(stream)
+            for t in tensors:
+                t.record_stream(here)
+        yield
+
+
+def _current_stream(t: torch.Tensor):
+    return torch.cuda.current_stream(t.device)
+
+
 class _Embedding(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, table, ids, scale, ignored, into):
+    def forward(ctx, table, ids, scale, ignored, into, node):
         ctx.save_for_backward(ids)
-        ctx.args = (table.shape[0], table.dtype, scale, ignored, into)
+        ctx.args = (table.shape[0], table.dtype, scale, ignored, into, node)
         return binding.themis_embedding_lookup(table, ids, scale)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, grad_out):
         (ids,) = ctx.saved_tensors
-        vocab, dtype, scale, ignored, into = ctx.args
+        vocab, dtype, scale, ignored, into, node = ctx.args
         if into is not None:
-            binding.themis_embedding_grad(grad_out, ids, vocab, scale, ignored, out=into, accumulate=True)
-            return None, None, None, None, None
+            _add_later(grad_out, ids, vocab, scale, ignored, into, node)
+            return None, None, None, None, None, None
         grad = binding.themis_embedding_grad(grad_out, ids, vocab, scale, ignored, out_dtype=dtype)
-        return grad, None, None, None, None
+        return grad, None, None, None, None, None
+
+
+def _add_later(grad_out, ids, vocab, scale, ignored, into, node):
+    """Adds the gradient to `into` where the table's own gradient is accumulated: behind whatever else
+    this backward accumulates there, on that stream, which the caller's waits for; and before hooks on the
+    accumulated gradient.  Where nothing is accumulated (a table that is not a leaf, torch.autograd.grad)
+    at the end of this backward, on the caller's stream."""
+    stream, task, left = _current_stream(grad_out), torch._C._current_graph_task_id(), [True]
+
+    def add():
+        if not left:
+            return
+        left.clear()
+        with _behind(stream, grad_out, ids):
+            binding.themis_embedding_grad(grad_out, ids, vocab, scale, ignored, out=into, accumulate=True)
+        torch.autograd.graph.increment_version(into)
+
+    def before_accumulation(_):
+        hook.remove()
+        if torch._C._current_graph_task_id() == task:   # (not so behind a backward that failed on its way)
+            add()
+
+    def at_the_end():
+        if hook is not None:
+            hook.remove()
+        add()
+
+    hook = node.register_prehook(before_accumulation) if node is not None else None
+    torch.autograd.Variable._execution_engine.queue_callback(at_the_end)
 
 
 def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, ignored: int = -1,
@@ -37,8 +83,13 @@ def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, ignore
 
     into: where the gradient is added in place of being returned to autograd (table.grad, say: a
     table that is also the output projection has one already, and only the rows of the tokens at
-    hand are touched).  Differentiable once: a derivative through the gradient raises an error."""
-    return _Embedding.apply(table, ids, float(scale), int(ignored), into)
+    hand are touched).  The addition is a change in place of `into` by every backward through the result,
+    torch.autograd.grad's among them, whose result for the table lacks it.  Differentiable once: a
+    derivative through the gradient raises an error."""
+    node = None
+    if into is not None and table.requires_grad and table.is_leaf and torch.is_grad_enabled():
+        node = torch.autograd.graph.get_gradient_edge(table).node
+    return _Embedding.apply(table, ids, float(scale), int(ignored), into, node)
 
 
 class GradientBuckets:
