@@ -549,7 +549,7 @@ int themis_embedding_lookup(const themis_rows_t *table, uint64_t vocab, uint64_t
  *               16-byte aligned, untouched until the stream has drained, one
  *               per call in flight.
  * vocab, n and width below 2^31, beyond 4,096 tokens width up to 2^24 and n times
- * width up to 2^38, else THEMIS_ERR_UNSUPPORTED.
+ * width up to 2^38, else THEMIS_ERR_UNSUPPORTED (and no workspace: 0 bytes).
  */
 size_t themis_embedding_grad_workspace_bytes(uint64_t n, uint64_t width, uint64_t vocab);
 int themis_embedding_grad(const themis_rows_t *grad_out, uint64_t width,

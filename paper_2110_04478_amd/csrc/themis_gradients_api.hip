@@ -111,6 +111,9 @@ GradLayout grad_layout(uint32_t n, uint32_t width, uint32_t vocab) {
   return l;
 }
 
+// What the grids of the sums and the joins hold: less than 2^32 lanes, 65,535 workgroups the other way.
+bool grad_fits(const GradLayout& l) { return (uint64_t)l.blocks * l.slabs <= 1u << 23 && l.slabs <= 65535; }
+
 void clear_table(Launches& go, const Rows& table, uint32_t width, uint32_t vocab) {
   if (table.inner == 0 && table.inner_stride == (int64_t)width) {
     const uint64_t bytes = (uint64_t)vocab * width * type_bytes(table.type);
@@ -178,7 +181,8 @@ int themis_embedding_lookup(const themis_rows_t* table, uint64_t vocab, uint64_t
 
 size_t themis_embedding_grad_workspace_bytes(uint64_t n, uint64_t width, uint64_t vocab) {
   if (n == 0 || width == 0 || vocab == 0 || n > kMost || width > kMost || vocab > kMost) return 0;
-  return grad_layout((uint32_t)n, (uint32_t)width, (uint32_t)vocab).bytes;
+  const GradLayout l = grad_layout((uint32_t)n, (uint32_t)width, (uint32_t)vocab);
+  return grad_fits(l) ? l.bytes : 0;
 }
 
 int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const themis_rows_t* ids, uint64_t n,
@@ -190,9 +194,9 @@ int themis_embedding_grad(const themis_rows_t* grad_out, uint64_t width, const t
   if (n > kMost || width > kMost || vocab > kMost) return THEMIS_ERR_UNSUPPORTED;
   if (!rows_apart(*grad, vocab, width)) return THEMIS_ERR_INVALID_ARGUMENT;
   const GradLayout l = grad_layout((uint32_t)n, (uint32_t)width, (uint32_t)vocab);
+  if (!grad_fits(l)) return THEMIS_ERR_UNSUPPORTED;
   if (l.bytes && (!workspace || workspace_bytes < l.bytes || !aligned(workspace, 16))) return THEMIS_ERR_WORKSPACE;
   const uint64_t sums = (uint64_t)l.blocks * l.slabs;
-  if (sums > 1u << 23 || l.slabs > 65535) return THEMIS_ERR_UNSUPPORTED;   // (grids of less than 2^32 lanes)
   const Rows g = n ? rows_of(*grad_out, n) : Rows{}, k = n ? rows_of(*ids, n) : Rows{}, to = rows_of(*grad, vocab);
   const uint32_t skip = ignored >= 0 && (uint64_t)ignored < vocab ? (uint32_t)ignored : ~0u;
   Launches go(stream);
