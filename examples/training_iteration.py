@@ -1,9 +1,9 @@
 """A training iteration's gradients, and how long a network takes to sum them.
 
 A small next-token model with a tied token table is trained for a few steps.  Every step looks
-tokens up, adds the table's gradient to the output projection's, takes the norm of all gradients
-and writes them, clipped, into the flat buckets that the ranks' All-Reduces carry; the parameters
-are updated from the buckets.  The sizes of the buckets are then a trace for the evaluator: it
+tokens up, adds the table's gradient to the output projection's, lays all gradients into the flat
+buckets that the ranks' All-Reduces carry, and clips what comes back by the norm of the sum; the
+parameters are updated from the buckets.  The sizes of the buckets are then a trace for the evaluator: it
 plans and simulates the iteration's All-Reduces on the six platforms of the paper's Table 2.
 
     python examples/training_iteration.py [steps]
@@ -69,7 +69,9 @@ def iteration_times(sizes, chunks=64):
     return np.stack(times)
 
 
-def main(steps=40, vocab=2000, width=256, batch=16, length=128, rate=2.0, max_norm=1.0, device="cuda:0"):
+def main(steps=40, vocab=2000, width=256, batch=16, length=128, rate=2.0, max_norm=1.0, device="cuda:0",
+         all_reduce=lambda buckets: None):
+    """all_reduce: sums the buckets over the ranks, in place (one rank: they are the sum)."""
     p = model(vocab, width, device, 1)
     buckets = GradientBuckets(p.values(), bucket_bytes=1 << 20)
     losses, norms = [], []
@@ -77,8 +79,9 @@ def main(steps=40, vocab=2000, width=256, batch=16, length=128, rate=2.0, max_no
         buckets.zero()
         loss = loss_of(p, batch_of(vocab, batch, length, device, step))
         loss.backward()
-        total, _ = buckets.clip(max_norm)
-        # (here the ranks' buckets would be summed)
+        buckets.fill()
+        all_reduce(buckets.buckets)
+        total, _ = buckets.clip_summed(max_norm)
         with torch.no_grad():
             for q in buckets.params:
                 q.sub_(buckets.views[q], alpha=rate)

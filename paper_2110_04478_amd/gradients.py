@@ -95,10 +95,15 @@ def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, ignore
 class GradientBuckets:
     """The gradients of a list of parameters, and the flat buckets that carry them.
 
+    The buckets hold the last parameter's gradient first, as gradients become ready, each at least
+    bucket_bytes unless it is the last.  Two ways to clip, which are the same on one rank only:
+
+        fill(); sum the buckets over the ranks; clip_summed(max_norm)   the norm of all ranks' sum
+        clip(max_norm); sum the buckets over the ranks                  each rank's own norm
+
     Every parameter gets a .grad of zeros that has to stay: zero_grad(set_to_none=True), a backward
-    with create_graph and moves of the module put others in its place, and clip() is an error until
-    zero() has put these back (after moves of the module: new buckets).  The buckets are filled in the order in which gradients become
-    ready, the last parameter's first, each with at least bucket_bytes unless it is the last."""
+    with create_graph and moves of the module put others in its place, and fill() and clip() are errors
+    until zero() has put these back (after moves of the module: new buckets)."""
 
     def __init__(self, params, bucket_bytes: int, dtype: torch.dtype = torch.bfloat16):
         self.params = [p for p in params if p.requires_grad]
@@ -120,7 +125,7 @@ class GradientBuckets:
             self.buckets.append(flat)
         self.plan = binding.themis_gradient_plan([p.grad for p in self.params],
                                                  [self.views[p] for p in self.params])
-
+        self.summed = binding.themis_gradient_plan([self.views[p] for p in self.params])
         self.places = [g.data_ptr() for g in self.plan.grads]
 
     def _stays(self) -> bool:
@@ -131,10 +136,23 @@ class GradientBuckets:
         for p, g in zip(self.params, self.plan.grads):
             p.grad = g.zero_()
 
-    def clip(self, max_norm: float):
-        """The clipped gradients into the buckets -> (f32[2]: norm and factor, norms of the
-        parameters' gradients f32[n])."""
+    def _need_gradients(self):
         binding._need(self._stays() and all(p.grad is g for p, g in zip(self.params, self.plan.grads)))
+
+    def fill(self):
+        """The gradients into the buckets as they are."""
+        self._need_gradients()
+        torch._foreach_copy_([self.views[p] for p in self.params], self.plan.grads)
+
+    def clip_summed(self, max_norm: float):
+        """What the buckets hold clipped in place -> (f32[2]: norm and factor, norms of the
+        parameters' parts f32[n])."""
+        return binding.themis_gradient_clip(self.summed, max_norm)
+
+    def clip(self, max_norm: float):
+        """This rank's gradients, clipped, into the buckets -> (f32[2]: norm and factor, norms of the
+        parameters' gradients f32[n])."""
+        self._need_gradients()
         return binding.themis_gradient_clip(self.plan, max_norm)
 
     def sizes(self) -> np.ndarray:

@@ -69,3 +69,17 @@ def test_gradients_that_were_moved(buckets):
     buckets.params[0].grad.data = torch.full((3,), 5.0)
     refused(lambda: buckets.clip(1.0))
     refused(buckets.zero)
+
+
+def test_filled_and_summed(buckets):
+    """The gradients as they are; the sum is clipped where it stands."""
+    buckets.zero()
+    backward(buckets.params)
+    buckets.fill()
+    assert torch.equal(buckets.buckets[0], torch.full((7,), 2.0)) and not buckets.clipped
+    buckets.buckets[0] *= 3.0                         # (three ranks alike)
+    buckets.clip_summed(1.0)
+    assert [c.tolist() for c in buckets.clipped[-1]] == [[6.0] * 3, [[6.0] * 2] * 2]
+    assert buckets.summed.out is None                 # in place
+    buckets.params[0].grad = None
+    refused(buckets.fill)
