@@ -601,9 +601,9 @@ def _targets_share(grads: list, outs: list) -> bool:
     for g, o in zip(grads, outs):
         if o.numel() == 0:
             continue
-        if overlap.repeats(o):
-            return True
         place = overlap.view_of(o)
+        if not o.is_contiguous() and overlap.repeats(o):
+            return True
         targets.append(place)
         if g is not o and (g.dtype != o.dtype or overlap.view_of(g) != place):
             others.append(overlap.view_of(g))

@@ -92,16 +92,20 @@ def repeats(t) -> bool:
 
 
 def _groups(spans):
-    """Numbers of the views whose spans (begin, end, number) hang together."""
+    """Numbers of the views whose spans (begin, end, number) hang together, two at least."""
     spans.sort()
-    group, reach = [], None
+    group, reach = [], -1
     for begin, end, i in spans:
-        if group and begin >= reach:
-            yield group
-            group = []
-        reach = end if not group else max(reach, end)
-        group.append(i)
-    if group:
+        if begin >= reach:
+            if len(group) > 1:
+                yield group
+            group = [i]
+            reach = end
+        else:
+            group.append(i)
+            if end > reach:
+                reach = end
+    if len(group) > 1:
         yield group
 
 
@@ -144,7 +148,12 @@ def shared(written, read) -> bool:
     """Whether a view of `written` has a byte in common with another one or with one of `read`
     (or the search for it is too long to say that it has not)."""
     views = [(*v, True) for v in written] + [(*v, False) for v in read]
-    spans = [(at, at + sum(s * n for s, n in levels) + size, i) for i, (at, levels, size, _) in enumerate(views)]
+    spans = []
+    for i, (at, levels, size, _) in enumerate(views):
+        end = at + size
+        for s, n in levels:
+            end += s * n
+        spans.append((at, end, i))
     steps = [_STEPS]
     try:
         return any(_share(views, g, None, steps) for g in _groups(spans))

@@ -50,7 +50,7 @@ def test_lists_with_gaps_that_share_elements():
     weight = torch.zeros(12, 16)
     windows = torch.zeros(64).as_strided((2, 2, 4), (6, 5, 1))
     for grads in ([base, base[:, :5]], [base[:, :5], base[:, 3:8]], [base, base.t()], [windows],
-                  [weight[:, :12].unfold(0, 4, 2)], [base[:6, :9], base[3:, :9]], [base[::2], base[::3]]):
+                  [weight[:, :12].unfold(0, 4, 2)], [base[:6, :9], base[3:, :9]], [base[::2], base[::3]], [base[:1, :3].expand(5, 3)]):
         assert binding._targets_share(grads, grads), [g.shape for g in grads]
     assert binding._targets_share([a, base], [base[:, :5], c])      # a target on another gradient
     assert binding._targets_share([base[:, :5]], [base[:, 1:6]])
