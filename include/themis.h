@@ -534,8 +534,8 @@ int themis_embedding_lookup(const themis_rows_t *table, uint64_t vocab, uint64_t
  * themis_embedding_grad -- the gradient of the table behind it:
  *   grad[v][j] = (accumulate ? grad[v][j] : 0) +
  *                scale * sum of grad_out[t][j] over the t with ids[t] == v
- * Sums are made in binary32 in an order that the token numbers alone decide,
- * and rounded once to grad's type.  Tokens of number `ignored` (padding; -1 for
+ * Sums are made in binary32 in an order that the token numbers, n and width
+ * decide, and rounded once to grad's type.  Tokens of number `ignored` (padding; -1 for
  * none) and those outside 0 .. vocab-1 have no gradient: their rows of grad_out
  * are not read.  Without `accumulate` every row of grad is written, those of
  * numbers that do not occur with zeros; with it, only rows of numbers that
@@ -562,7 +562,8 @@ int themis_embedding_grad(const themis_rows_t *grad_out, uint64_t width,
  * c * in_col_stride].  A tensor may be given as several parts (one after the
  * other, the same `tensor`): more dimensions than two, say.  out may be in
  * itself (same type and strides), NULL where only norms are wanted, or memory
- * of any of the three types that overlaps no other part.
+ * of any of the three types that overlaps no other part.  That an out gives no
+ * element twice is checked part by part; parts are not compared with each other.
  */
 typedef struct themis_gradient {
   const void *in;
@@ -609,8 +610,8 @@ int themis_gradient_plan(const themis_gradient_t *parts, uint64_t n_parts, uint6
  *   out = in * factor,   factor = max_norm / total if total > max_norm, else 1
  *   total[1] = factor
  * The product is made in binary32 and rounded once to out's type.  With a NaN
- * norm the factor is NaN, with an infinite one 0.  max_norm is positive and
- * finite.  Gradients that are their own out are left alone where the factor
+ * norm the factor is NaN, with an infinite one 0; below 2^-126 it has the fewer
+ * bits of binary32's subnormal numbers.  max_norm is positive and finite.  Gradients that are their own out are left alone where the factor
  * is 1.
  *
  *   workspace : plan->workspace_bytes, 16-byte aligned, untouched until the

@@ -241,10 +241,12 @@ few_tokens_kernel(uint32_t n, Rows grad_out, uint32_t width, Rows ids, float sca
 // Sort: least significant digit first, up to ten bits a pass and two launches: every workgroup
 // counts the digits of its part of the list, then every workgroup finds from all counts where its
 // part's tokens go.  A token's key is its number, or `vocab` (behind all others) if it has no
-// gradient.  Bound by waits: of 16,384 tokens the four launches take 17 us, of 131,072 26 us.
+// gradient.  Bound by waits: of 16,384 tokens the four launches take 20 us, of 131,072 27 us.
 //
-// Sums: bound by memory.  131,072 tokens of 2,048 bf16 added to 65,536 binary32 rows (0.96 GB) take
-// 222 us without the sort, 4.3 TB/s; 16,384 tokens of 4,096 into a cleared table of 131,072 rows 55.
+// Sums: bound by memory and, a step of eight tokens after the other, by the waits for keys, then rows.
+// 131,072 tokens of 2,048 bf16 added to 65,536 binary32 rows (0.96 GB) take 222 us without the sort,
+// 4.3 TB/s, where a plain pass of three reads and a write makes 5.95; 16,384 tokens of 4,096 into a
+// cleared table of 131,072 rows 61 (2.9 TB/s).
 // A tile is 32 tokens: with 16 more sums cross tiles (65,537 tokens, half of them one number: 113 us,
 // 107), with 64 the longest workgroups end late (131,072 tokens of 1,024 131 us, 122).
 // ---------------------------------------------------------------------------

@@ -6,6 +6,9 @@
 // binary64: a conversion and a fused multiply-add per element, a tenth of what the vector units
 // can issue while the elements come from memory, and no scaling against overflow is needed.
 //
+// What is not one run of elements goes element by element, with a division each: three column slices
+// of 4,096^2 bf16 take 83 us (dense 24), 162 when they are clipped (57).
+//
 // Clipping is a second launch, in which every workgroup adds the first one's sums again, in the same
 // order (8 KiB), and takes the pieces from the last to the first.  Bound by memory: the norm of
 // 1.74 G bf16 elements 499 us, 7.0 TB/s; 1.07 G binary32 elements into bf16 1,730 us, 6.2 TB/s of
