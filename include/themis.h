@@ -622,6 +622,132 @@ int themis_gradient_norm(const themis_gradient_plan_t *plan, float *total, float
 int themis_gradient_clip(const themis_gradient_plan_t *plan, double max_norm, float *total,
                          float *norms, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * An expert layer of the iteration, and dropout
+ *
+ * Between the token table and the gradients: a gate gives every token k of
+ * n_experts experts, the tokens' rows are put in the order of their experts, and
+ * what the experts make of them is summed per token.  With a capacity every
+ * expert has a buffer of one size, so that the bytes of an exchange between
+ * ranks are known before any token is.  The conventions are those above.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * themis_expert_gate -- the k largest logits of every token and their softmax:
+ *   experts[t][j] = number of the j-th largest of logits[t], the lower of equals
+ *   weights[t][j] = exp(logits[t][experts[t][j]]) / sum of exp(logits[t][e]) over
+ *                   the k chosen e (renormalize), or over all e
+ * made in binary32 and rounded once.  A logit of -inf is never chosen: where a
+ * token has fewer than k others the rest of its experts are -1, of weight 0.
+ * (Finite logits, the type's lowest too, are chosen like any other.)  A NaN is
+ * larger than every number; a NaN or +inf makes the token's weights NaN.
+ *
+ * themis_expert_gate_grad -- the gradient of the logits behind it, the choice held:
+ *   grad_logits[t][e] = sum over j with experts[t][j] == e of w_j grad_weights[t][j]
+ *                       - p_e * sum over j of w_j grad_weights[t][j]
+ * with w_j as above before rounding and p_e the softmax over the chosen
+ * (renormalize; 0 elsewhere), or over all.  Numbers outside 0 .. n_experts-1
+ * have no part; a number that stands twice counts twice.
+ *
+ *   logits, grad_logits   : n rows of n_experts, THEMIS_F32 / _BF16 / _F16
+ *   weights, grad_weights : n rows of k, any of the three types
+ *   experts               : n rows of k, THEMIS_I32 / _I64
+ * What is written must overlap nothing else.  n below 2^31, n_experts up to
+ * 1,024, k up to 64, else THEMIS_ERR_UNSUPPORTED; k is not above n_experts in
+ * themis_expert_gate.
+ */
+int themis_expert_gate(const themis_rows_t *logits, uint64_t n_experts, uint64_t n, uint64_t k,
+                       int renormalize, const themis_rows_t *weights,
+                       const themis_rows_t *experts, void *stream);
+int themis_expert_gate_grad(const themis_rows_t *grad_weights, const themis_rows_t *logits,
+                            uint64_t n_experts, const themis_rows_t *experts, uint64_t n,
+                            uint64_t k, int renormalize, const themis_rows_t *grad_logits,
+                            void *stream);
+
+/*
+ * The order of n * k pairs (token t, its j-th expert) by expert, in slots:
+ * packed (capacity 0), n * k slots, the experts' pairs end to end; or n_experts *
+ * capacity slots, those of expert e from e * capacity on.  An expert's pairs stand in the order
+ * of t * k + j; those beyond its capacity have no slot, nor have those
+ * of numbers outside 0 .. n_experts-1.
+ */
+typedef struct themis_expert_order {
+  uint64_t n, k, n_experts, capacity;
+  int32_t *place;  /* [n][k] slot of a pair, -1 for none                      */
+  int32_t *counts; /* [n_experts] pairs of an expert, those without a slot too */
+  int32_t *starts; /* [n_experts + 1] first slot of an expert; behind the last */
+  int32_t *source; /* [slots] the pair of a slot, t * k + j, -1 for none      */
+} themis_expert_order_t;
+
+/*
+ * themis_expert_sort -- fills in place, counts, starts and source.
+ *
+ *   experts   : n rows of k numbers, THEMIS_I32 / _I64
+ *   workspace : themis_expert_sort_workspace_bytes(n, k, n_experts) bytes, 16-byte
+ *               aligned, untouched until the stream has drained, one per call in
+ *               flight.
+ * n * k and the slots below 2^31, n_experts up to 1,024, else
+ * THEMIS_ERR_UNSUPPORTED (and no workspace: 0 bytes).
+ */
+size_t themis_expert_sort_workspace_bytes(uint64_t n, uint64_t k, uint64_t n_experts);
+int themis_expert_sort(const themis_rows_t *experts, const themis_expert_order_t *order,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * themis_expert_dispatch -- rows into the order:
+ *   out[s] = x[source[s] / k], zeros in the slots of no pair
+ * themis_expert_combine -- and back:
+ *   out[t] = (accumulate ? out[t] : 0) + sum over j of weights[t][j] * y[place[t][j]]
+ * over the pairs that have a slot, in the order of j, in binary32, rounded once;
+ * weights NULL: 1.  Without weights and accumulate it is the gradient of
+ * themis_expert_dispatch.  Rows of slots of no pair are not read.
+ * themis_expert_combine_grad -- the gradients of y and of the weights behind it:
+ *   grad_y[s]          = weights[t][j] * grad_out[t] for the pair of slot s, zeros
+ *                        in the slots of no pair
+ *   grad_weights[t][j] = sum of grad_out[t][c] * y[place[t][j]][c], 0 without a slot
+ * Either may be NULL.  (Without weights the gradient of y is
+ * themis_expert_dispatch of grad_out.)
+ *
+ *   order          : as themis_expert_sort filled it; place and source are read, and
+ *                    a place or source that is none of the order's is taken as -1
+ *   x, out of combine, grad_out   : n rows of `width`, any of the three types
+ *   out of dispatch, y, grad_y    : a row for every slot; grad_y of y's type
+ *   weights, grad_weights         : n rows of k, any of the three types
+ * What is written must overlap nothing else.  width up to 2^25, else
+ * THEMIS_ERR_UNSUPPORTED.
+ */
+int themis_expert_dispatch(const themis_expert_order_t *order, const themis_rows_t *x,
+                           uint64_t width, const themis_rows_t *out, void *stream);
+int themis_expert_combine(const themis_expert_order_t *order, const themis_rows_t *y,
+                          uint64_t width, const themis_rows_t *weights, int accumulate,
+                          const themis_rows_t *out, void *stream);
+int themis_expert_combine_grad(const themis_expert_order_t *order, const themis_rows_t *grad_out,
+                               uint64_t width, const themis_rows_t *y,
+                               const themis_rows_t *weights, const themis_rows_t *grad_y,
+                               const themis_rows_t *grad_weights, void *stream);
+
+/*
+ * themis_dropout -- elements dropped with probability p, the others scaled:
+ *   out[r][c] = add[r][c] + (dropped(r, c) ? 0 : x[r][c] / (1 - p))
+ * in binary32 with the factor 1 / (1 - p), rounded once; add NULL: 0.  The mask
+ * is a function of (seed, call, r, c) and is never stored, so that the gradient is the same
+ * call on grad_out without add: with w = word c % 4 of Philox4x32-10 (Salmon et
+ * al., 2011) on the counter (c / 4, r, call's low and high half) under the key
+ * (seed's low and high half), an element is dropped if w < p * 2^32, rounded to
+ * nearest.  A dropped element is 0 whatever x holds.
+ *
+ *   call_at : NULL, or a device address whose number is added to `call` when the
+ *             kernel runs: a captured graph draws another mask in every replay if
+ *             the number is moved on between them.  8-byte aligned.
+ *   x       : n rows of `width`, any of the three types; add has out's type.
+ *   out     : may be x or add themselves (same type and strides), else its rows
+ *             must overlap neither.
+ * p is 0 .. 1; n below 2^31, width up to 2^25, else THEMIS_ERR_UNSUPPORTED.
+ */
+int themis_dropout(const themis_rows_t *x, uint64_t n, uint64_t width, double p, uint64_t seed,
+                   uint64_t call, const uint64_t *call_at, const themis_rows_t *add,
+                   const themis_rows_t *out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -54,6 +54,11 @@ class _GradientPlan(C.Structure):
                 ("strided", C.c_uint32), ("image", _vp)]
 
 
+class _ExpertOrder(C.Structure):
+    _fields_ = [("n", C.c_uint64), ("k", C.c_uint64), ("n_experts", C.c_uint64), ("capacity", C.c_uint64),
+                ("place", _vp), ("counts", _vp), ("starts", _vp), ("source", _vp)]
+
+
 _lib = None
 
 
@@ -125,6 +130,25 @@ def lib():
         L.themis_gradient_clip.restype = C.c_int
         L.themis_gradient_clip.argtypes = [C.POINTER(_GradientPlan), C.c_double, _vp, _vp, _vp,
                                            C.c_size_t, _vp]
+        rows, order = C.POINTER(_Rows), C.POINTER(_ExpertOrder)
+        L.themis_expert_gate.restype = C.c_int
+        L.themis_expert_gate.argtypes = [rows, C.c_uint64, C.c_uint64, C.c_uint64, C.c_int, rows, rows, _vp]
+        L.themis_expert_gate_grad.restype = C.c_int
+        L.themis_expert_gate_grad.argtypes = [rows, rows, C.c_uint64, rows, C.c_uint64, C.c_uint64, C.c_int,
+                                              rows, _vp]
+        L.themis_expert_sort_workspace_bytes.restype = C.c_size_t
+        L.themis_expert_sort_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.c_uint64]
+        L.themis_expert_sort.restype = C.c_int
+        L.themis_expert_sort.argtypes = [rows, order, _vp, C.c_size_t, _vp]
+        L.themis_expert_dispatch.restype = C.c_int
+        L.themis_expert_dispatch.argtypes = [order, rows, C.c_uint64, rows, _vp]
+        L.themis_expert_combine.restype = C.c_int
+        L.themis_expert_combine.argtypes = [order, rows, C.c_uint64, rows, C.c_int, rows, _vp]
+        L.themis_expert_combine_grad.restype = C.c_int
+        L.themis_expert_combine_grad.argtypes = [order, rows, C.c_uint64, rows, rows, rows, rows, _vp]
+        L.themis_dropout.restype = C.c_int
+        L.themis_dropout.argtypes = [rows, C.c_uint64, C.c_uint64, C.c_double, C.c_uint64, C.c_uint64, _vp, rows,
+                                     rows, _vp]
         _lib = L
     return _lib
 
@@ -401,6 +425,7 @@ def alloc_workspace(nbytes: int, device="cuda:0") -> Optional[torch.Tensor]:
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int32: 3, torch.int64: 4}
 INVALID_ARGUMENT = -1
+UNSUPPORTED = -2
 
 
 def _rows(t: torch.Tensor, lead: int, width: int) -> Optional[_Rows]:
@@ -671,3 +696,254 @@ def themis_gradient_clip(plan: GradientPlan, max_norm: float):
     _check(lib().themis_gradient_clip(plan.c_struct, max_norm, at, at + 8, plan.workspace_at,
                                       plan.c_struct.workspace_bytes, plan.stream()))
     return torch.split_with_sizes(result, (2, plan.n_tensors))
+
+
+# -- an expert layer of the iteration, and dropout ----------------------------------------
+
+def _result(given: Optional[torch.Tensor], like: torch.Tensor, shape, dtype: Optional[torch.dtype]) -> torch.Tensor:
+    """`given`, checked, or a new tensor of this shape and type (like's where none is named)."""
+    if given is None:
+        _need(dtype is None or dtype in _FLOATS)
+        return like.new_empty(shape, dtype=dtype)
+    _need(given.dtype in _FLOATS and given.shape == shape and given.get_device() == like.get_device() and
+          dtype in (None, given.dtype))
+    return given
+
+
+def _need_apart(out: Optional[torch.Tensor], *inputs):
+    """What the caller gave to be written shares no memory with what is read."""
+    if out is not None:
+        for t in inputs:
+            if t is not None and _one_storage(out, t):
+                _need(_apart(out, t))
+
+
+def _written_rows(t: torch.Tensor, width: int) -> _Rows:
+    r = _rows(t, t.dim() - 1, width)
+    _need(r is not None)
+    return r
+
+
+def themis_expert_gate(logits: torch.Tensor, k: int, renormalize: bool = True,
+                       out_dtype: torch.dtype = torch.float32, index_dtype: torch.dtype = torch.int32) -> tuple:
+    """The k largest of the last dimension, equal ones in ascending order -> (weights [.., k]: their
+    softmax, over the chosen alone or (renormalize=False) over all; experts [.., k]).  A logit of
+    -inf is not chosen: a token with fewer than k others has experts -1 of weight 0 behind them."""
+    device = logits.get_device()
+    _need(device >= 0 and logits.dim() >= 1 and logits.dtype in _FLOATS and out_dtype in _FLOATS and
+          index_dtype in _INDEXES)
+    n_experts = logits.shape[-1]
+    _need(0 <= k <= n_experts)
+    shape = (*logits.shape[:-1], k)
+    weights = logits.new_empty(shape, dtype=out_dtype)
+    experts = logits.new_empty(shape, dtype=index_dtype)
+    if weights.numel() == 0:
+        return weights, experts
+    stream = _stream_here(device)
+    n = weights.numel() // k
+    rows_l, logits = _read_rows(logits, len(shape) - 1, n_experts)
+    _check(lib().themis_expert_gate(rows_l, n_experts, n, k, int(renormalize), _written_rows(weights, k),
+                                    _written_rows(experts, k), stream))
+    return weights, experts
+
+
+def themis_expert_gate_grad(grad_weights: torch.Tensor, logits: torch.Tensor, experts: torch.Tensor,
+                            renormalize: bool = True, out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """The gradient of the logits behind themis_expert_gate, of the logits' type unless out_dtype
+    says another."""
+    device = logits.get_device()
+    _need(device >= 0 and logits.dim() >= 1 and logits.dtype in _FLOATS and grad_weights.dtype in _FLOATS and
+          experts.dtype in _INDEXES and experts.dim() == logits.dim() and
+          experts.shape[:-1] == logits.shape[:-1] and grad_weights.shape == experts.shape and
+          grad_weights.get_device() == device and experts.get_device() == device and
+          out_dtype in (None, *_FLOATS))
+    grad = torch.empty(logits.shape, dtype=out_dtype or logits.dtype, device=logits.device)
+    if grad.numel() == 0:
+        return grad
+    stream = _stream_here(device)
+    lead, n_experts, k = logits.dim() - 1, logits.shape[-1], experts.shape[-1]
+    rows_g, grad_weights = _read_rows(grad_weights, lead, k)
+    rows_l, logits = _read_rows(logits, lead, n_experts)
+    rows_e, experts = _read_rows(experts, lead, k)
+    _check(lib().themis_expert_gate_grad(rows_g, rows_l, n_experts, rows_e, grad.numel() // n_experts, k,
+                                         int(renormalize), _written_rows(grad, n_experts), stream))
+    return grad
+
+
+@dataclass
+class ExpertOrder:
+    """Pairs (token, its j-th expert) in the order of their experts (themis_expert_sort)."""
+    place: torch.Tensor    # i32 [.., k]: slot of a pair, -1 for none
+    counts: torch.Tensor   # i32 [n_experts]: pairs of an expert, those without a slot too
+    starts: torch.Tensor   # i32 [n_experts + 1]: first slot of an expert; behind the last
+    source: torch.Tensor   # i32 [slots]: the pair of a slot, token * k + j, -1 for none
+    capacity: int          # slots of an expert; 0: packed
+    c_struct: _ExpertOrder
+    streams: set           # raw handles: the one it was made on, and others that have used it
+
+    @property
+    def shape(self):
+        """Of the tokens."""
+        return self.place.shape[:-1]
+
+    @property
+    def slots(self) -> int:
+        return self.source.shape[0]
+
+    def stream(self) -> int:
+        """The current stream; the order's memory, once it is given up, waits for it."""
+        stream = _stream_here(self.place.get_device())
+        if stream not in self.streams:
+            self.streams.add(stream)
+            for t in (self.place, self.counts, self.starts, self.source):
+                t.record_stream(torch.cuda.current_stream())
+        return stream
+
+
+def themis_expert_sort(experts: torch.Tensor, n_experts: int, capacity: int = 0,
+                       workspace: Optional[torch.Tensor] = None) -> ExpertOrder:
+    """Orders the pairs of experts [.., k] by expert, an expert's in the tokens' order.
+
+    capacity 0: the experts' pairs end to end, as many slots as pairs; else a buffer of this many
+    slots for every expert, whose later pairs have none.  Numbers outside 0 .. n_experts-1 have no slot."""
+    device = experts.get_device()
+    _need(device >= 0 and experts.dim() >= 1 and experts.dtype in _INDEXES and n_experts >= 1 and capacity >= 0 and
+          (workspace is None or (workspace.get_device() == device and workspace.is_contiguous())))
+    stream = _stream_here(device)
+    k, pairs = experts.shape[-1], experts.numel()
+    n = pairs // k if k else experts.shape[:-1].numel()
+    slots = n_experts * capacity if capacity else pairs
+    if max(n, k, pairs, slots, n_experts) >= 1 << 31:
+        raise ThemisError(UNSUPPORTED)
+    new = functools.partial(torch.empty, dtype=torch.int32, device=experts.device)
+    order = _ExpertOrder(n, k, n_experts, capacity)
+    # (one allocation for all four: a call on a few tokens is the host's time)
+    place, counts, starts, source = torch.split_with_sizes(new(pairs + 2 * n_experts + 1 + slots),
+                                                           (pairs, n_experts, n_experts + 1, slots))
+    order.place, order.counts, order.starts, order.source = (t.data_ptr() for t in (place, counts, starts, source))
+    need = lib().themis_expert_sort_workspace_bytes(n, k, n_experts)
+    if workspace is None and need:
+        workspace = alloc_workspace(need, experts.device)
+    at, size = (None, 0) if workspace is None else (workspace.data_ptr(),
+                                                    workspace.numel() * workspace.element_size())
+    rows_e, experts = _read_rows(experts, experts.dim() - 1, k)
+    _check(lib().themis_expert_sort(rows_e, order, at, size, stream))
+    return ExpertOrder(place.view(experts.shape), counts, starts, source, capacity, order, {stream})
+
+
+def _need_rows_of(order: ExpertOrder, t: torch.Tensor, shape):
+    """t has these rows and is on the order's device."""
+    _need(t.dtype in _FLOATS and t.dim() == len(shape) + 1 and t.shape[:-1] == shape and
+          t.get_device() == order.place.get_device())
+
+
+def themis_expert_dispatch(x: torch.Tensor, order: ExpertOrder, out: Optional[torch.Tensor] = None,
+                           out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """The tokens' rows x [.., width] in the order of their experts -> [slots, width] of out's type
+    (given by out or out_dtype; x's otherwise), zeros in the slots of no pair.  Its gradient is
+    themis_expert_combine without weights."""
+    _need_rows_of(order, x, order.shape)
+    width = x.shape[-1]
+    result = _result(out, x, (order.slots, width), out_dtype)
+    if result.numel() == 0:
+        return result
+    _need_apart(out, x, order.place, order.source)
+    stream = order.stream()
+    rows_x, x = _read_rows(x, x.dim() - 1, width)
+    _check(lib().themis_expert_dispatch(order.c_struct, rows_x, width, _written_rows(result, width), stream))
+    return result
+
+
+def themis_expert_combine(y: torch.Tensor, order: ExpertOrder, weights: Optional[torch.Tensor] = None,
+                          out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                          accumulate: bool = False) -> torch.Tensor:
+    """The sum of a token's rows of y [slots, width], times weights [.., k] -> [.., width] of out's
+    type (given by out or out_dtype; y's otherwise), or added to out where `accumulate`.  Pairs
+    without a slot have no part."""
+    _need_rows_of(order, y, (order.slots,))
+    if weights is not None:
+        _need_rows_of(order, weights, order.shape)
+        _need(weights.shape == order.place.shape)
+    _need(out is not None or not accumulate)
+    width = y.shape[-1]
+    result = _result(out, y, (*order.shape, width), out_dtype)
+    if result.numel() == 0:
+        return result
+    _need_apart(out, y, weights, order.place)
+    stream = order.stream()
+    rows_y, y = _read_rows(y, 1, width)
+    rows_w = None
+    if weights is not None:
+        rows_w, weights = _read_rows(weights, weights.dim() - 1, weights.shape[-1])
+    _check(lib().themis_expert_combine(order.c_struct, rows_y, width, rows_w, int(accumulate),
+                                       _written_rows(result, width), stream))
+    return result
+
+
+def themis_expert_combine_grad(grad_out: torch.Tensor, y: torch.Tensor, order: ExpertOrder, weights: torch.Tensor,
+                               need_rows: bool = True, need_weights: bool = True) -> tuple:
+    """The gradients behind themis_expert_combine with weights -> (of y [slots, width], of the
+    weights [.., k]), each of its tensor's type, None where it is not needed."""
+    _need_rows_of(order, grad_out, order.shape)
+    _need_rows_of(order, y, (order.slots,))
+    _need_rows_of(order, weights, order.shape)
+    width = y.shape[-1]
+    _need(grad_out.shape[-1] == width and weights.shape == order.place.shape)
+    stream = order.stream()
+    rows = torch.empty(y.shape, dtype=y.dtype, device=y.device) if need_rows else None
+    products = torch.empty(weights.shape, dtype=weights.dtype, device=y.device) if need_weights else None
+    rows_g, grad_out = _read_rows(grad_out, grad_out.dim() - 1, width)
+    rows_y, y = _read_rows(y, 1, width)
+    rows_w, weights = _read_rows(weights, weights.dim() - 1, weights.shape[-1])
+    _check(lib().themis_expert_combine_grad(order.c_struct, rows_g, width, rows_y, rows_w,
+                                            _written_rows(rows, width) if need_rows else None,
+                                            _written_rows(products, products.shape[-1]) if need_weights else None,
+                                            stream))
+    return rows, products
+
+
+def _in_place(a: torch.Tensor, b: torch.Tensor) -> bool:
+    return a.data_ptr() == b.data_ptr() and a.dtype == b.dtype and a.shape == b.shape and a.stride() == b.stride()
+
+
+def themis_dropout(x: torch.Tensor, p: float, seed: int, call, add: Optional[torch.Tensor] = None,
+                   out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """add + x / (1 - p), elements of x dropped with probability p -> out's type (given by out,
+    which may be x or add themselves, or out_dtype; add's or x's otherwise).
+
+    What is dropped is a function of (seed, call, row, column), x as rows of its last dimension: the
+    gradient of x is the same call on the result's gradient, without add.  call: a whole number, or a
+    tensor of one 64 bit number on the GPU, read when the kernel runs (a captured graph draws another mask in
+    every replay if the program moves it on)."""
+    device = x.get_device()
+    given = out is not None
+    _need(device >= 0 and x.dim() >= 1 and x.dtype in _FLOATS and 0.0 <= p <= 1.0)
+    if add is not None:
+        _need(add.shape == x.shape and add.dtype in _FLOATS and add.get_device() == device)
+        out_dtype = out_dtype or (None if given else add.dtype)
+    call_at = None
+    if isinstance(call, torch.Tensor):
+        _need(call.dtype == torch.int64 and call.numel() == 1 and call.get_device() == device)
+        call, call_at = 0, call
+    out = _result(out, x, x.shape, out_dtype)
+    _need(add is None or add.dtype == out.dtype)
+    if out.numel() == 0:
+        return out
+    if given:
+        for t in (x, add):
+            if t is not None and _one_storage(out, t) and not _in_place(out, t):
+                _need(_apart(out, t))
+        _need_apart(out, call_at)
+    stream = _stream_here(device)
+    lead, width = x.dim() - 1, x.shape[-1]
+    rows_o = _written_rows(out, width)
+    rows_x, x = _read_rows(x, lead, width)
+    rows_a = None
+    if add is not None:
+        rows_a, add = _read_rows(add, lead, width)
+    _check(lib().themis_dropout(rows_x, x.numel() // width, width, p, seed & _ALL64, call & _ALL64,
+                                None if call_at is None else call_at.data_ptr(), rows_a, rows_o, stream))
+    return out
+
+
+_ALL64 = (1 << 64) - 1

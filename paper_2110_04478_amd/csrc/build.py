@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 PKG = os.path.dirname(HERE)
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libthemis_hip.so")
-SOURCES = [os.path.join(HERE, "themis_api.hip"), os.path.join(HERE, "themis_gradients_api.hip")]
+SOURCES = [os.path.join(HERE, name + ".hip") for name in ("themis_api", "themis_gradients_api", "themis_experts_api")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -99,6 +99,15 @@ struct Access {
     for (uint32_t k = 1; k < kVec; ++k)
       if (k >= skip) row[at + k] = (T)v[k];
   }
+  // Zero in the places of other lanes' elements.
+  template <bool kWhole>
+  __device__ __forceinline__ Floats<kVec> own(Floats<kVec> v) const {
+    if (count == kVec) return v;
+#pragma unroll
+    for (uint32_t k = 0; k < kVec; ++k)
+      if (kWhole ? k < skip || !count : k >= count) v[k] = 0.0f;
+    return v;
+  }
   // Where lanes that share elements, or have none of their own, write what the owner writes.
   template <bool kWhole, bool kAway, typename T>
   __device__ __forceinline__ void write_over(T* row, Floats<kVec> v) const {
@@ -125,6 +134,8 @@ struct Slice<8> {
   __device__ __forceinline__ typename Packed<T, 8>::type read(const T* row) const { return a.read<kWhole>(row); }
   template <bool kWhole, typename T>
   __device__ __forceinline__ void write(T* row, float8 v) const { a.write<kWhole>(row, v); }
+  template <bool kWhole>
+  __device__ __forceinline__ float8 own(float8 v) const { return a.own<kWhole>(v); }
   template <bool kWhole, bool kAway, typename T>
   __device__ __forceinline__ void write_over(T* row, float8 v) const { a.write_over<kWhole, kAway>(row, v); }
 };
@@ -142,6 +153,10 @@ struct Slice<4> {
   __device__ __forceinline__ void write(T* row, float8 v) const {
     a.write<kWhole>(row, v.lo);
     b.write<kWhole>(row, v.hi);
+  }
+  template <bool kWhole>
+  __device__ __forceinline__ float8 own(float8 v) const {
+    return __builtin_shufflevector(a.own<kWhole>(v.lo), b.own<kWhole>(v.hi), 0, 1, 2, 3, 4, 5, 6, 7);
   }
   template <bool kWhole, bool kAway, typename T>
   __device__ __forceinline__ void write_over(T* row, float8 v) const {
@@ -175,6 +190,22 @@ __device__ __forceinline__ int64_t row_offset(const Rows& rows, uint32_t r) {
 template <typename T>
 __device__ __forceinline__ T* row_at(const Rows& rows, uint32_t r) {
   return (T*)rows.data + row_offset(rows, r);
+}
+
+// Zeros in the rows of `empty` behind v0, by a workgroup: short rows side by side.  kAway: past the
+// caches (beside sums that need them: 65,537 tokens of 1,000 108 us, through them 116; alone it is
+// 200 MB in 52 us and 45).
+template <bool kWhole, bool kAway, typename Out>
+__device__ __forceinline__ void write_zeros(uint64_t empty, uint32_t v0, uint32_t width, const Rows& grad) {
+  constexpr int kVec = kVecOf<Out>;
+  const uint32_t vecs = (width + kVec - 1) / kVec;
+  const uint32_t shift = vecs >= 256 ? 8u : vecs <= 1 ? 0u : 32u - (uint32_t)__builtin_clz(vecs - 1);
+  for (uint32_t r = threadIdx.x >> shift; r < 64; r += 256u >> shift) {
+    if (!((empty >> r) & 1u)) continue;
+    Out* to = row_at<Out>(grad, v0 + r);
+    for (uint32_t c = threadIdx.x & ((1u << shift) - 1u); c < vecs; c += 256)
+      Access<kVec>(c * kVec, width).template write_over<kWhole, kAway>(to, Floats<kVec>(0.0f));
+  }
 }
 
 // Numbers of the tokens t[] as table rows, ~0u for those outside the table; the loads are in flight

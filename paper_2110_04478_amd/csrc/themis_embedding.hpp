@@ -86,22 +86,6 @@ __device__ __forceinline__ float8 sum_listed(const Slice<kVec>& slice, const Row
   return sum;
 }
 
-// Zeros in the rows of `empty` behind v0, by a workgroup: short rows side by side.  kAway: past the
-// caches (beside sums that need them: 65,537 tokens of 1,000 108 us, through them 116; alone it is
-// 200 MB in 52 us and 45).
-template <bool kWhole, bool kAway, typename Out>
-__device__ __forceinline__ void write_zeros(uint64_t empty, uint32_t v0, uint32_t width, const Rows& grad) {
-  constexpr int kVec = kVecOf<Out>;
-  const uint32_t vecs = (width + kVec - 1) / kVec;
-  const uint32_t shift = vecs >= 256 ? 8u : vecs <= 1 ? 0u : 32u - (uint32_t)__builtin_clz(vecs - 1);
-  for (uint32_t r = threadIdx.x >> shift; r < 64; r += 256u >> shift) {
-    if (!((empty >> r) & 1u)) continue;
-    Out* to = row_at<Out>(grad, v0 + r);
-    for (uint32_t c = threadIdx.x & ((1u << shift) - 1u); c < vecs; c += 256)
-      Access<kVec>(c * kVec, width).template write_over<kWhole, kAway>(to, Floats<kVec>(0.0f));
-  }
-}
-
 // Zeros in a whole table, before the sums.  One store a lane: workgroups that end at once follow each
 // other through memory, and nothing is waited for (1 GiB: 7.1 TB/s; in loops over 16 KiB to 1 MiB, or
 // behind a look at whether a row is needed, 4 to 6).

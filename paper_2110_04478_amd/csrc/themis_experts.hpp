@@ -1,0 +1,564 @@
+// An expert layer's operators on the rank: the gate, the order of tokens by expert, rows into that
+// order and back (themis_expert_*).
+#pragma once
+
+#include "themis_elements.hpp"
+
+namespace themis {
+
+// ---------------------------------------------------------------------------
+// Over the 2^shift lanes of a group (aligned, up to a wavefront; all lanes are on): a sum, the same in
+// every lane and every call, and the largest and smallest value.
+// ---------------------------------------------------------------------------
+template <typename F>
+__device__ __forceinline__ uint32_t over_group(uint32_t x, uint32_t shift, F f) {
+  if (shift > 0) x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, false));    // lane ^ 1
+  if (shift > 1) x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, false));    // lane ^ 2
+  if (shift > 2) x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, false));   // 7 - lane
+  if (shift > 3) x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xF, 0xF, false));   // 15 - lane
+  if (shift > 4) {   // rows of 16 lanes, two and two, then the halves
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = f(r[0], r[1]);
+  }
+  if (shift > 5) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = f(r[0], r[1]);
+  }
+  return x;
+}
+__device__ __forceinline__ float group_sum(float x, uint32_t shift) {
+  return __uint_as_float(over_group(__float_as_uint(x), shift, [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
+__device__ __forceinline__ uint32_t group_max(uint32_t x, uint32_t shift) {
+  return over_group(x, shift, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+__device__ __forceinline__ uint32_t group_min(uint32_t x, uint32_t shift) {
+  return over_group(x, shift, [](uint32_t a, uint32_t b) { return min(a, b); });
+}
+
+// One element of a row of any type.
+__device__ __forceinline__ float float_at(const Rows& rows, uint32_t r, uint32_t j) {
+  const int64_t at = row_offset(rows, r) + j;
+  if (rows.type == THEMIS_F32) return ((const float*)rows.data)[at];
+  if (rows.type == THEMIS_BF16) return (float)((const __bf16*)rows.data)[at];
+  return (float)((const _Float16*)rows.data)[at];
+}
+__device__ __forceinline__ void put_float(const Rows& rows, uint32_t r, uint32_t j, float x) {
+  const int64_t at = row_offset(rows, r) + j;
+  if (rows.type == THEMIS_F32) ((float*)rows.data)[at] = x;
+  else if (rows.type == THEMIS_BF16) ((__bf16*)rows.data)[at] = (__bf16)x;
+  else ((_Float16*)rows.data)[at] = (_Float16)x;
+}
+// A number of 0 .. most-1, or ~0u.
+__device__ __forceinline__ uint32_t number_at(const Rows& rows, uint32_t r, uint32_t j, uint32_t most) {
+  const int64_t at = row_offset(rows, r) + j;
+  const int64_t x = rows.type == THEMIS_I64 ? ((const int64_t*)rows.data)[at] : ((const int32_t*)rows.data)[at];
+  return (uint64_t)x < most ? (uint32_t)x : ~0u;
+}
+__device__ __forceinline__ void put_number(const Rows& rows, uint32_t r, uint32_t j, int32_t x) {
+  const int64_t at = row_offset(rows, r) + j;
+  if (rows.type == THEMIS_I64) ((int64_t*)rows.data)[at] = x;
+  else ((int32_t*)rows.data)[at] = x;
+}
+
+// ---------------------------------------------------------------------------
+// themis_expert_gate: the k largest logits of a token and their softmax.
+//
+// 2^shift lanes take a token, each kOwn adjacent logits in registers; k times the largest is found
+// (over a lane's own, then over the lanes) and taken out.  Logits are compared as whole numbers
+// that are ordered as the values are; those of 16 bits carry their index in the lower half, smaller ones
+// first, so that one maximum gives both.
+// ---------------------------------------------------------------------------
+constexpr uint32_t kMostExperts = 1024;
+constexpr uint32_t kMostChosen = 64;
+constexpr uint32_t kGateLeastShift = 3;   // (32 tokens a workgroup at most: the results wait in LDS)
+
+// A logit as a key: NaN above all, -0 as 0.  No element: 0.  first(): of what may be chosen.
+template <typename T>
+struct LogitKey {   // 16 bits
+  static constexpr bool kIndexed = true;
+  static __device__ __forceinline__ uint32_t of(T x, uint32_t index) {
+    uint32_t b = __builtin_bit_cast(uint16_t, x);
+    b = x != x ? 0x7FFFu : b == 0x8000u ? 0u : b;
+    return (b & 0x8000u ? ~b & 0xFFFFu : b | 0x8000u) << 16 | (0xFFFFu - index);
+  }
+  static __device__ __forceinline__ float value(uint32_t key) {
+    const uint32_t s = key >> 16, b = s & 0x8000u ? s & 0x7FFFu : ~s & 0xFFFFu;
+    return (float)__builtin_bit_cast(T, (uint16_t)b);
+  }
+  static __device__ __forceinline__ uint32_t index(uint32_t key) { return 0xFFFFu - (key & 0xFFFFu); }
+  static __device__ __forceinline__ uint32_t first() { return of(-(T)__builtin_inff(), 0) + 1; }
+};
+template <>
+struct LogitKey<float> {
+  static constexpr bool kIndexed = false;
+  static __device__ __forceinline__ uint32_t of(float x, uint32_t) {
+    uint32_t b = __float_as_uint(x);
+    b = x != x ? 0x7FFFFFFFu : b == 0x80000000u ? 0u : b;
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+  }
+  static __device__ __forceinline__ float value(uint32_t key) {
+    return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+  }
+  static __device__ __forceinline__ uint32_t first() { return of(-__builtin_inff(), 0) + 1; }
+};
+
+// A lane's kOwn logits from `first` on, `none` behind the last one.
+template <int kOwn, typename T>
+__device__ __forceinline__ typename Packed<T, kOwn>::type own_logits(const T* row, uint32_t first, uint32_t experts, T none) {
+  if (first + kOwn <= experts) return load<kOwn>(row + first);
+  typename Packed<T, kOwn>::type v = none;
+#pragma unroll
+  for (uint32_t i = 0; i + 1 < kOwn; ++i)
+    if (first + i < experts) v[i] = row[first + i];
+  return v;
+}
+
+template <typename T, int kOwn>
+__global__ void __launch_bounds__(256)
+gate_kernel(Rows logits, uint32_t experts, uint32_t n, uint32_t k, bool renormalize, Rows weights, Rows chosen,
+            uint32_t shift) {
+  typedef LogitKey<T> Key;
+  __shared__ uint32_t best[(256 >> kGateLeastShift) * kMostChosen];
+  __shared__ int32_t number[(256 >> kGateLeastShift) * kMostChosen];
+  const uint32_t lanes = 1u << shift, lane = threadIdx.x & (lanes - 1u), group = threadIdx.x >> shift;
+  const uint32_t groups = 256u >> shift, own = lane * kOwn;
+  for (uint64_t at = (uint64_t)blockIdx.x * groups; at < n; at += (uint64_t)gridDim.x * groups) {
+    const uint32_t t = (uint32_t)at + group;
+    const T* row = row_at<const T>(logits, min(t, n - 1u));
+    const auto v = own_logits<kOwn>(row, own, experts, (T)-__builtin_inff());
+    uint32_t key[kOwn];
+#pragma unroll
+    for (uint32_t i = 0; i < kOwn; ++i) key[i] = own + i < experts ? Key::of(v[i], own + i) : 0u;
+    float largest = -__builtin_inff();
+    for (uint32_t j = 0; j < k; ++j) {
+      uint32_t top = key[0];
+#pragma unroll
+      for (uint32_t i = 1; i < kOwn; ++i) top = max(top, key[i]);
+      top = group_max(top, shift);
+      uint32_t index;
+      if constexpr (Key::kIndexed) {
+        index = Key::index(top);
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; ++i) key[i] = key[i] == top ? 0u : key[i];
+      } else {
+        index = ~0u;
+#pragma unroll
+        for (uint32_t i = kOwn; i-- > 0;) index = key[i] == top ? own + i : index;
+        index = group_min(index, shift);
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; ++i) key[i] = own + i == index ? 0u : key[i];
+      }
+      const bool any = top >= Key::first();
+      if (j == 0 && any) largest = Key::value(top);
+      if (lane == 0) {
+        best[group * k + j] = top;
+        number[group * k + j] = any ? (int32_t)index : -1;
+      }
+    }
+    float sum = 0.0f;
+    if (!renormalize) {
+#pragma unroll
+      for (uint32_t i = 0; i < kOwn; ++i) sum += own + i < experts ? expf((float)v[i] - largest) : 0.0f;
+      sum = group_sum(sum, shift);
+    }
+    __syncthreads();
+    if (renormalize) {
+      for (uint32_t j = lane; j < k; j += lanes)
+        if (number[group * k + j] >= 0) sum += expf(Key::value(best[group * k + j]) - largest);
+      sum = group_sum(sum, shift);
+    }
+    if (t < n)
+      for (uint32_t j = lane; j < k; j += lanes) {
+        const int32_t e = number[group * k + j];
+        put_number(chosen, t, j, e);
+        put_float(weights, t, j, e < 0 ? 0.0f : expf(Key::value(best[group * k + j]) - largest) / sum);
+      }
+    __syncthreads();   // (the next tokens' results)
+  }
+}
+
+// ---------------------------------------------------------------------------
+// themis_expert_gate_grad.  With w the weights and p the softmax over all logits:
+//   over the chosen:  dl[e] = sum over j with e_j == e of w_j (dw_j - sum_i w_i dw_i)
+//   over all:         dl[e] = sum over j with e_j == e of w_j dw_j  -  p_e sum_i w_i dw_i
+// The lanes of a token hold its logits as in the gate, and a pair (expert, gradient) each, which is handed
+// round; an expert that stands twice in a token's list is added twice, in order.
+// ---------------------------------------------------------------------------
+template <typename T, typename Out, int kOwn>
+__global__ void __launch_bounds__(256)
+gate_grad_kernel(Rows grad, Rows logits, uint32_t experts, Rows chosen, uint32_t n, uint32_t k, bool renormalize, Rows out,
+                 uint32_t shift) {
+  const uint32_t lanes = 1u << shift, lane = threadIdx.x & (lanes - 1u), group = threadIdx.x >> shift;
+  const uint32_t groups = 256u >> shift, own = lane * kOwn;
+  const float none = -__builtin_inff();
+  for (uint64_t at = (uint64_t)blockIdx.x * groups; at < n; at += (uint64_t)gridDim.x * groups) {
+    const uint32_t t0 = (uint32_t)at + group, t = min(t0, n - 1u);
+    const T* row = row_at<const T>(logits, t);
+    const auto v = own_logits<kOwn>(row, own, experts, (T)none);
+    struct Pair { uint32_t expert; float logit, grad; };
+    auto pair_of = [&](uint32_t j) {
+      Pair p = {~0u, none, 0.0f};
+      if (j < k) p.expert = number_at(chosen, t, j, experts);
+      if (p.expert != ~0u) {
+        p.logit = (float)row[p.expert];
+        p.grad = float_at(grad, t, j);
+      }
+      return p;
+    };
+    const Pair first = pair_of(lane);
+    uint32_t top = 0;   // as a key, so that a NaN is not lost
+    if (renormalize) {
+      for (uint32_t j = lane; j < k; j += lanes)
+        top = max(top, LogitKey<float>::of(j == lane ? first.logit : pair_of(j).logit, 0));
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < kOwn; ++i) top = max(top, LogitKey<float>::of((float)v[i], 0));
+    }
+    top = group_max(top, shift);
+    const bool any = top >= LogitKey<float>::first();
+    const float largest = any ? LogitKey<float>::value(top) : 0.0f;
+    float sum = 0.0f, dot = 0.0f, e[kOwn];
+#pragma unroll
+    for (uint32_t i = 0; i < kOwn; ++i) {
+      e[i] = renormalize ? 0.0f : expf((float)v[i] - largest);
+      sum += e[i];
+    }
+    for (uint32_t j = lane; j < k; j += lanes) {
+      const Pair p = j == lane ? first : pair_of(j);
+      if (p.expert == ~0u) continue;
+      const float w = expf(p.logit - largest);
+      if (renormalize) sum += w;
+      dot += w * p.grad;
+    }
+    sum = group_sum(sum, shift);
+    dot = group_sum(dot, shift);
+    dot = any ? dot / sum : 0.0f;
+#pragma unroll
+    for (uint32_t i = 0; i < kOwn; ++i) e[i] = renormalize || !any ? 0.0f : -(e[i] / sum) * dot;
+    for (uint32_t j0 = 0; j0 < k; j0 += lanes) {
+      const Pair p = j0 == 0 ? first : pair_of(j0 + lane);
+      const float w = any ? expf(p.logit - largest) / sum : 0.0f;
+      const float mine = p.expert == ~0u ? 0.0f : w * (renormalize ? p.grad - dot : p.grad);
+      const uint32_t some = min(k - j0, lanes);
+      for (uint32_t j = 0; j < some; ++j) {
+        const int from = (int)((threadIdx.x & 63u & ~(lanes - 1u)) + j);
+        const uint32_t place = (uint32_t)__shfl((int)p.expert, from) - own;
+        const float add = __shfl(mine, from);
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; ++i) e[i] += place == i ? add : 0.0f;
+      }
+    }
+    if (t0 < n) {
+      Out* to = row_at<Out>(out, t);
+      if (own + kOwn <= experts) {
+        Floats<kOwn> x;
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; ++i) x[i] = e[i];
+        store<kOwn>(to + own, x);
+      } else {
+#pragma unroll
+        for (uint32_t i = 0; i + 1 < kOwn; ++i)
+          if (own + i < experts) to[own + i] = (Out)e[i];
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// themis_expert_sort: pairs (token, expert) by expert, stable.
+//
+// As the table gradient's sort, in one pass: the workgroups count the experts of their parts of the
+// list, then every workgroup finds from all counts where its part's pairs go.  One workgroup does both
+// where the list is short.
+// ---------------------------------------------------------------------------
+struct Order {
+  uint32_t n, k, pairs, experts, capacity, slots;   // capacity 0: packed
+  int32_t *place, *counts, *starts, *source;
+};
+
+constexpr uint32_t kPairGroup = 1024, kPairWaves = kPairGroup / 64;
+constexpr uint32_t kPairsAhead = 4;    // of a lane in flight
+constexpr uint32_t kPartsAhead = 16;   // counts
+
+// Experts of the pairs a[] (token * k + j), ~0u for none.
+template <int kPairs>
+__device__ __forceinline__ void experts_of(const Order& o, const Rows& chosen, const uint32_t (&a)[kPairs],
+                                           uint32_t (&expert)[kPairs]) {
+  if (!chosen.inner && chosen.inner_stride == (int64_t)o.k) {   // one run of numbers
+    const Rows run = {chosen.data, 0, 1, 0, chosen.type};
+    token_rows(run, a, o.experts, expert);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) expert[i] = number_at(chosen, a[i] / o.k, a[i] % o.k, o.experts);
+}
+
+__device__ __forceinline__ void count_expert(uint32_t* bins, uint32_t expert, bool on) {
+  if (on) atomicAdd(&bins[expert], 1u);
+}
+
+__global__ void __launch_bounds__(kPairGroup)
+expert_count_kernel(Order o, Rows chosen, uint32_t part, uint32_t* counts) {
+  __shared__ uint32_t count[kMostExperts];
+  const uint32_t first = blockIdx.x * part, last = min(first + part, o.pairs);
+  for (uint32_t b = threadIdx.x; b < o.experts; b += kPairGroup) count[b] = 0;
+  __syncthreads();
+  for (uint32_t i = first + threadIdx.x; i < last; i += kPairsAhead * kPairGroup) {
+    uint32_t at[kPairsAhead], expert[kPairsAhead];
+#pragma unroll
+    for (uint32_t k = 0; k < kPairsAhead; ++k) at[k] = min(i + k * kPairGroup, last - 1u);
+    experts_of(o, chosen, at, expert);
+#pragma unroll
+    for (uint32_t k = 0; k < kPairsAhead; ++k)
+      count_expert(count, expert[k], i + k * kPairGroup < last && expert[k] != ~0u);
+  }
+  __syncthreads();
+  for (uint32_t b = threadIdx.x; b < o.experts; b += kPairGroup) counts[blockIdx.x * o.experts + b] = count[b];
+}
+
+__global__ void __launch_bounds__(kPairGroup)
+expert_sort_kernel(Order o, Rows chosen, uint32_t part, uint32_t parts, const uint32_t* counts, uint32_t bits) {
+  __shared__ uint32_t next[kPairWaves][kMostExperts];   // first a wavefront's counts, then where its next one goes
+  __shared__ uint32_t wave_sums[kPairWaves];
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
+  const uint32_t first = blockIdx.x * part, share = part / kPairWaves;   // (a multiple of 64)
+  const uint32_t begin = min(first + wave * share, o.pairs), end = min(begin + share, o.pairs);
+  const uint32_t b = threadIdx.x;   // a lane has one expert, or none
+  if (b < o.experts)
+#pragma unroll
+    for (uint32_t w = 0; w < kPairWaves; ++w) next[w][b] = 0;
+  __syncthreads();
+  for (uint32_t i = begin; i < end; i += kPairsAhead * 64) {
+    uint32_t at[kPairsAhead], expert[kPairsAhead];
+#pragma unroll
+    for (uint32_t k = 0; k < kPairsAhead; ++k) at[k] = min(i + k * 64 + lane, end - 1u);
+    experts_of(o, chosen, at, expert);
+#pragma unroll
+    for (uint32_t k = 0; k < kPairsAhead; ++k)
+      count_expert(next[wave], expert[k], i + k * 64 + lane < end && expert[k] != ~0u);
+  }
+  uint32_t before = 0, all = 0;   // of this lane's expert: in the parts before, in all
+  if (parts > 1 && b < o.experts) {
+    for (uint32_t p = 0; p < parts; p += kPartsAhead) {
+      uint32_t c[kPartsAhead];
+#pragma unroll
+      for (uint32_t k = 0; k < kPartsAhead; ++k) c[k] = counts[min(p + k, parts - 1u) * o.experts + b];
+#pragma unroll
+      for (uint32_t k = 0; k < kPartsAhead; ++k) {
+        before += p + k < blockIdx.x ? c[k] : 0u;
+        all += p + k < parts ? c[k] : 0u;
+      }
+    }
+  }
+  __syncthreads();   // (the wavefronts' counts are complete)
+  if (parts == 1 && b < o.experts)
+#pragma unroll
+    for (uint32_t w = 0; w < kPairWaves; ++w) all += next[w][b];
+  uint32_t upto = all;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t y = __shfl_up(upto, d);
+    if (lane >= (uint32_t)d) upto += y;
+  }
+  if (lane == 63) wave_sums[wave] = upto;
+  __syncthreads();
+  uint32_t start = upto - all, total = 0;   // where the expert's pairs begin; how many pairs have an expert
+#pragma unroll
+  for (uint32_t w = 0; w < kPairWaves; ++w) {
+    start += w < wave ? wave_sums[w] : 0u;
+    total += wave_sums[w];
+  }
+  if (o.capacity) start = b * o.capacity;
+  if (b < o.experts) {
+    uint32_t at = before;   // (counted from the expert's first)
+#pragma unroll
+    for (uint32_t w = 0; w < kPairWaves; ++w) {
+      const uint32_t c = next[w][b];
+      next[w][b] = at;
+      at += c;
+    }
+  }
+  __shared__ uint32_t starts[kMostExperts];
+  if (b < o.experts) starts[b] = start;
+  if (blockIdx.x == 0) {
+    if (b < o.experts) {
+      o.counts[b] = (int32_t)all;
+      o.starts[b] = (int32_t)start;
+    }
+    if (b == 0) o.starts[o.experts] = (int32_t)(o.capacity ? o.slots : total);
+  }
+  __syncthreads();
+  for (uint32_t i0 = begin; i0 < end; i0 += kPairsAhead * 64) {
+    uint32_t from[kPairsAhead], expert[kPairsAhead];
+#pragma unroll
+    for (uint32_t k = 0; k < kPairsAhead; ++k) from[k] = min(i0 + k * 64 + lane, end - 1u);
+    experts_of(o, chosen, from, expert);
+#pragma unroll
+    for (uint32_t k = 0; k < kPairsAhead; ++k) {
+      if (i0 + k * 64 >= end) break;
+      const bool in = i0 + k * 64 + lane < end, on = in && expert[k] != ~0u;
+      uint64_t same = __ballot(on);   // lanes with this lane's expert
+      for (uint32_t x = 0; x < bits; ++x) {
+        const uint64_t ones = __ballot((expert[k] >> x) & 1u);
+        same &= (expert[k] >> x) & 1u ? ones : ~ones;
+      }
+      const uint32_t rank = (uint32_t)__popcll(same & ((1ull << lane) - 1));
+      // (all lanes have read before the first of an expert's adds: a wavefront's accesses to LDS are
+      // served in the order of the program, and these are kept in it)
+      uint32_t* seat = &next[wave][on ? expert[k] : 0u];
+      const uint32_t to = (on ? __hip_atomic_load(seat, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0u) + rank;
+      if (on && rank == 0)
+        __hip_atomic_store(seat, to + (uint32_t)__popcll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      const bool kept = on && (!o.capacity || to < o.capacity);
+      const uint32_t slot = kept ? starts[expert[k]] + to : ~0u;
+      if (in) o.place[from[k]] = (int32_t)slot;
+      if (kept) o.source[slot] = (int32_t)from[k];
+    }
+  }
+  // Slots of no pair.
+  if (!o.capacity) {
+    for (uint64_t s = total + (uint64_t)blockIdx.x * kPairGroup + threadIdx.x; s < o.slots; s += (uint64_t)parts * kPairGroup)
+      o.source[s] = -1;
+    return;
+  }
+  __shared__ uint32_t filled[kMostExperts];
+  if (b < o.experts) filled[b] = all;
+  __syncthreads();
+  for (uint64_t e = blockIdx.x * kPairWaves + wave; e < o.experts; e += (uint64_t)parts * kPairWaves)
+    for (uint64_t s = (uint64_t)filled[e] + lane; s < o.capacity; s += 64) o.source[e * o.capacity + s] = -1;
+}
+
+// ---------------------------------------------------------------------------
+// Rows into the order of the experts and back.  2^shift lanes take a token's row (a chunk of 2,048
+// elements of a longer one: blockIdx.y), each eight elements.  A place that is no slot (-1, or what a
+// caller wrote there) is none.
+// ---------------------------------------------------------------------------
+
+// Zeros in the slots of no pair, by workgroup `block` of `blocks`.
+template <bool kWhole, typename Out>
+__device__ __forceinline__ void clear_empty_slots(const Order& o, uint32_t block, uint32_t blocks, uint32_t rows,
+                                                  uint32_t width, const Rows& out) {
+  const uint32_t lane = threadIdx.x & 63u;
+  for (uint64_t s0 = (uint64_t)block * rows; s0 < o.slots; s0 += (uint64_t)blocks * rows) {
+    const uint32_t s = (uint32_t)s0 + lane;
+    const bool empty = lane < rows && s < o.slots && (uint32_t)o.source[min(s, o.slots - 1u)] >= o.pairs;
+    write_zeros<kWhole, true, Out>(__ballot(empty), (uint32_t)s0, width, out);
+  }
+}
+
+// themis_expert_dispatch: a row is read once and written to its token's slots; the first `fills`
+// workgroups clear the slots of no pair.
+template <bool kWhole, typename In, typename Out>
+__global__ void __launch_bounds__(256)
+dispatch_kernel(Order o, Rows x, uint32_t width, Rows out, uint32_t shift, uint32_t fills, uint32_t fill_rows) {
+  if (blockIdx.x < fills) {
+    if (blockIdx.y == 0) clear_empty_slots<kWhole, Out>(o, blockIdx.x, fills, fill_rows, width, out);
+    return;
+  }
+  const uint32_t lanes = 1u << shift, groups = 256u >> shift, block = blockIdx.x - fills, blocks = gridDim.x - fills;
+  const Slice<kVecOf<In, Out>> slice(blockIdx.y * 256u * kLaneElements, threadIdx.x & (lanes - 1u), lanes, width);
+  if (!slice.any()) return;
+  for (uint64_t t = (uint64_t)block * groups + (threadIdx.x >> shift); t < o.n; t += (uint64_t)blocks * groups) {
+    const int32_t* place = o.place + t * o.k;
+    const float8 v = widen<8>(slice.template read<kWhole>(row_at<const In>(x, (uint32_t)t)));
+    for (uint32_t j = 0; j < o.k; ++j) {
+      const uint32_t s = (uint32_t)place[j];
+      if (s < o.slots) slice.template write_over<kWhole, true>(row_at<Out>(out, s), v);
+    }
+  }
+}
+
+// themis_expert_combine: out[t] (+)= sum over j of weights[t][j] * y[place[t][j]], kAhead rows in flight.
+constexpr uint32_t kCombineAhead = 4;
+template <bool kWhole, typename In, typename Out>
+__global__ void __launch_bounds__(256)
+combine_kernel(Order o, Rows y, uint32_t width, Rows weights, bool accumulate, Rows out, uint32_t shift) {
+  const uint32_t lanes = 1u << shift, groups = 256u >> shift;
+  const Slice<kVecOf<In, Out>> slice(blockIdx.y * 256u * kLaneElements, threadIdx.x & (lanes - 1u), lanes, width);
+  if (!slice.any()) return;
+  for (uint64_t t = (uint64_t)blockIdx.x * groups + (threadIdx.x >> shift); t < o.n; t += (uint64_t)gridDim.x * groups) {
+    const int32_t* place = o.place + t * o.k;
+    float8 sum = 0.0f;
+    for (uint32_t j0 = 0; j0 < o.k; j0 += kCombineAhead) {
+      uint32_t s[kCombineAhead];
+      float w[kCombineAhead];
+      typename Packed<In, 8>::type v[kCombineAhead];
+#pragma unroll
+      for (uint32_t u = 0; u < kCombineAhead; ++u) {
+        const uint32_t j = min(j0 + u, o.k - 1u);
+        s[u] = j0 + u < o.k ? (uint32_t)place[j] : ~0u;
+        w[u] = weights.data ? float_at(weights, (uint32_t)t, j) : 1.0f;
+      }
+#pragma unroll
+      for (uint32_t u = 0; u < kCombineAhead; ++u) {
+        v[u] = {};
+        if (s[u] < o.slots) v[u] = slice.template read<kWhole>(row_at<const In>(y, s[u]));
+      }
+#pragma unroll
+      for (uint32_t u = 0; u < kCombineAhead; ++u)
+        if (s[u] < o.slots) sum += widen<8>(v[u]) * w[u];
+    }
+    Out* to = row_at<Out>(out, (uint32_t)t);
+    if (accumulate) sum += widen<8>(slice.template read<kWhole>((const Out*)to));
+    slice.template write<kWhole>(to, sum);
+  }
+}
+
+// themis_expert_combine_grad: rows[s] = weights[a] * grad[t] and weights'[a] = <grad[t], y[s]> for the pair
+// a = (t, j) in slot s.  2^shift lanes (up to a wavefront) take kPairs of a token's pairs over the whole
+// row, so that a product is summed where it is made.
+template <bool kWhole, typename G, typename Y, int kPairs>
+__global__ void __launch_bounds__(256)
+combine_grad_kernel(Order o, Rows grad, uint32_t width, Rows y, Rows weights, Rows rows, Rows grad_weights, uint32_t shift,
+                    uint32_t fills, uint32_t fill_rows) {
+  if (blockIdx.x < fills) {
+    clear_empty_slots<kWhole, Y>(o, blockIdx.x, fills, fill_rows, width, rows);
+    return;
+  }
+  const uint32_t lanes = 1u << shift, lane = threadIdx.x & (lanes - 1u), each = (o.k + kPairs - 1) / kPairs;
+  const uint32_t groups = 256u >> shift, block = blockIdx.x - fills, blocks = gridDim.x - fills;
+  const uint64_t units = (uint64_t)o.n * each;
+  for (uint64_t u0 = (uint64_t)block * groups; u0 < units; u0 += (uint64_t)blocks * groups) {
+    const uint64_t unit = u0 + (threadIdx.x >> shift);
+    const bool mine = unit < units;
+    const uint32_t t = mine ? (uint32_t)(unit / each) : 0u, j0 = mine ? (uint32_t)(unit % each) * kPairs : 0u;
+    uint32_t s[kPairs];
+    float w[kPairs], dot[kPairs];
+#pragma unroll
+    for (uint32_t u = 0; u < kPairs; ++u) {
+      const uint32_t j = min(j0 + u, o.k - 1u);
+      s[u] = mine && j0 + u < o.k ? (uint32_t)o.place[(uint64_t)t * o.k + j] : ~0u;
+      w[u] = float_at(weights, t, j);
+      dot[u] = 0.0f;
+    }
+    for (uint32_t c = 0; c < width; c += lanes * kLaneElements) {
+      const Slice<kVecOf<G, Y>> slice(c, lane, lanes, width);
+      if (!slice.any()) continue;
+      const float8 g = widen<8>(slice.template read<kWhole>(row_at<const G>(grad, t)));
+      typename Packed<Y, 8>::type v[kPairs];
+#pragma unroll
+      for (uint32_t u = 0; u < kPairs; ++u) {
+        v[u] = {};
+        if (grad_weights.data && s[u] < o.slots) v[u] = slice.template read<kWhole>(row_at<const Y>(y, s[u]));
+      }
+#pragma unroll
+      for (uint32_t u = 0; u < kPairs; ++u) {
+        if (s[u] >= o.slots) continue;
+        if (rows.data) slice.template write_over<kWhole, true>(row_at<Y>(rows, s[u]), g * w[u]);
+        const float8 p = slice.template own<kWhole>(g * widen<8>(v[u]));
+        dot[u] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      }
+    }
+    if (!grad_weights.data) continue;
+#pragma unroll
+    for (uint32_t u = 0; u < kPairs; ++u) {
+      const float sum = group_sum(dot[u], shift);
+      if (mine && lane == 0 && j0 + u < o.k) put_float(grad_weights, t, j0 + u, sum);
+    }
+  }
+}
+
+}  // namespace themis

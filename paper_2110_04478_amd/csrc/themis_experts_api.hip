@@ -1,0 +1,263 @@
+// C ABI of the expert layer's operators and of dropout (see include/themis.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "themis.h"
+#include "themis_dropout.hpp"
+#include "themis_elements.hpp"
+#include "themis_experts.hpp"
+#include "themis_launch.hpp"
+
+namespace themis {
+namespace {
+
+constexpr uint64_t kMostWidth = 1u << 25;   // (in chunks of 1,024: what a grid takes the other way)
+
+// Lanes of a token's logits, 2^shift of `own` each.
+struct GateLayout { uint32_t own, shift; };
+GateLayout gate_layout(uint32_t experts) {
+  GateLayout l = {8, kGateLeastShift};
+  if (experts > 512) l = {16, 6};
+  else if (experts > 64) l.shift = next_power((experts + 7) / 8);
+  else l.own = experts <= 8 ? 1 : experts <= 16 ? 2 : experts <= 32 ? 4 : 8;
+  return l;
+}
+template <typename F>
+void with_own(uint32_t own, F&& f) {
+  if (own == 1) f(std::integral_constant<int, 1>{});
+  else if (own == 2) f(std::integral_constant<int, 2>{});
+  else if (own == 4) f(std::integral_constant<int, 4>{});
+  else if (own == 8) f(std::integral_constant<int, 8>{});
+  else f(std::integral_constant<int, 16>{});
+}
+
+uint32_t blocks_of(uint64_t n, uint64_t each) { return (uint32_t)std::min<uint64_t>((n + each - 1) / each, 1u << 20); }
+
+// Pairs of a workgroup and workgroups of the sort.
+struct SortLayout { uint32_t part, parts; size_t bytes; };
+SortLayout sort_layout(uint32_t pairs, uint32_t experts) {
+  SortLayout l = {kPairGroup, 1, 0};
+  while ((uint64_t)pairs > (uint64_t)l.part * (40 * (l.part / kPairGroup))) l.part *= 2;
+  l.parts = std::max(1u, (pairs + l.part - 1) / l.part);
+  if (l.parts > 1) l.bytes = (size_t)l.parts * experts * sizeof(uint32_t);
+  return l;
+}
+
+// Sizes and addresses of an order; its view.
+int order_status(const themis_expert_order_t* o, Order& view) {
+  if (!o || o->n_experts == 0) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (o->n_experts > kMostExperts || o->n > kMost || o->k > kMost || o->capacity > kMost) return THEMIS_ERR_UNSUPPORTED;
+  const uint64_t pairs = o->n * o->k, slots = o->capacity ? o->n_experts * o->capacity : pairs;
+  if (pairs > kMost || slots > kMost) return THEMIS_ERR_UNSUPPORTED;
+  view = {(uint32_t)o->n, (uint32_t)o->k, (uint32_t)pairs, (uint32_t)o->n_experts, (uint32_t)o->capacity, (uint32_t)slots,
+          o->place, o->counts, o->starts, o->source};
+  if ((pairs && (!o->place || !aligned(o->place, 4))) || (slots && (!o->source || !aligned(o->source, 4))))
+    return THEMIS_ERR_INVALID_ARGUMENT;
+  return THEMIS_OK;
+}
+
+// Rows that are written: n of `width` elements.
+bool target_ok(const themis_rows_t* r, uint64_t n, uint64_t width, bool index = false) {
+  return rows_ok(r, index) && rows_apart(*r, n, width);
+}
+
+// How a row of `width` elements is spread over lanes and columns of workgroups.
+struct RowLayout { uint32_t shift, chunks; };
+RowLayout row_layout(uint64_t width, uint32_t vec = kLaneElements) {
+  const uint32_t vecs = (uint32_t)((width + vec - 1) / vec);
+  return {std::min(next_power(vecs), 8u), (vecs + 255) / 256};
+}
+
+// Slots of a workgroup that looks for those of no pair: about 256 KiB.
+uint32_t slots_to_clear(uint64_t row_bytes) {
+  return (uint32_t)std::min<uint64_t>(64, std::max<uint64_t>(1, (256u << 10) / row_bytes));
+}
+
+Rows rows_or_none(const themis_rows_t* r, uint64_t n) { return r ? rows_of(*r, n) : Rows{}; }
+
+}  // namespace
+}  // namespace themis
+
+using namespace themis;
+
+extern "C" {
+
+int themis_expert_gate(const themis_rows_t* logits, uint64_t n_experts, uint64_t n, uint64_t k, int renormalize,
+                       const themis_rows_t* weights, const themis_rows_t* experts, void* stream) {
+  if (k > n_experts) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (n == 0 || k == 0) return THEMIS_OK;
+  if (!rows_ok(logits, false) || !rows_ok(weights, false) || !rows_ok(experts, true)) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (n > kMost || n_experts > kMostExperts || k > kMostChosen) return THEMIS_ERR_UNSUPPORTED;
+  if (!rows_apart(*weights, n, k) || !rows_apart(*experts, n, k)) return THEMIS_ERR_INVALID_ARGUMENT;
+  const GateLayout l = gate_layout((uint32_t)n_experts);
+  Launches go(stream);
+  with_type(logits->type, [&](auto in) {
+    with_own(l.own, [&](auto own) {
+      go(gate_kernel<decltype(in), decltype(own)::value>, dim3(blocks_of(n, 256u >> l.shift)), 256, rows_of(*logits, n),
+         (uint32_t)n_experts, (uint32_t)n, (uint32_t)k, renormalize != 0, rows_of(*weights, n), rows_of(*experts, n),
+         l.shift);
+    });
+  });
+  return go.status();
+}
+
+int themis_expert_gate_grad(const themis_rows_t* grad_weights, const themis_rows_t* logits, uint64_t n_experts,
+                            const themis_rows_t* experts, uint64_t n, uint64_t k, int renormalize,
+                            const themis_rows_t* grad_logits, void* stream) {
+  if (n == 0 || n_experts == 0) return THEMIS_OK;
+  if (!rows_ok(logits, false) || !rows_ok(grad_logits, false)) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (k && (!rows_ok(grad_weights, false) || !rows_ok(experts, true))) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (n > kMost || n_experts > kMostExperts || k > kMostChosen) return THEMIS_ERR_UNSUPPORTED;
+  if (!rows_apart(*grad_logits, n, n_experts)) return THEMIS_ERR_INVALID_ARGUMENT;
+  const GateLayout l = gate_layout((uint32_t)n_experts);
+  const Rows g = k ? rows_of(*grad_weights, n) : Rows{}, e = k ? rows_of(*experts, n) : Rows{};
+  Launches go(stream);
+  with_type(logits->type, [&](auto in) {
+    with_type(grad_logits->type, [&](auto out) {
+      with_own(l.own, [&](auto own) {
+        go(gate_grad_kernel<decltype(in), decltype(out), decltype(own)::value>, dim3(blocks_of(n, 256u >> l.shift)), 256, g,
+           rows_of(*logits, n), (uint32_t)n_experts, e, (uint32_t)n, (uint32_t)k, renormalize != 0,
+           rows_of(*grad_logits, n), l.shift);
+      });
+    });
+  });
+  return go.status();
+}
+
+size_t themis_expert_sort_workspace_bytes(uint64_t n, uint64_t k, uint64_t n_experts) {
+  if (n > kMost || k > kMost || n * k > kMost || n_experts == 0 || n_experts > kMostExperts) return 0;
+  return sort_layout((uint32_t)(n * k), (uint32_t)n_experts).bytes;
+}
+
+int themis_expert_sort(const themis_rows_t* experts, const themis_expert_order_t* order, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  Order o;
+  if (const int status = order_status(order, o)) return status;
+  if (o.pairs && !rows_ok(experts, true)) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (!o.counts || !o.starts || !aligned(o.counts, 4) || !aligned(o.starts, 4)) return THEMIS_ERR_INVALID_ARGUMENT;
+  const SortLayout l = sort_layout(o.pairs, o.experts);
+  if (l.bytes && (!workspace || workspace_bytes < l.bytes || !aligned(workspace, 16))) return THEMIS_ERR_WORKSPACE;
+  const Rows chosen = o.pairs ? rows_of(*experts, o.n) : Rows{};
+  uint32_t* counts = (uint32_t*)workspace;
+  Launches go(stream);
+  if (l.parts > 1) go(expert_count_kernel, dim3(l.parts), kPairGroup, o, chosen, l.part, counts);
+  go(expert_sort_kernel, dim3(l.parts), kPairGroup, o, chosen, l.part, l.parts, (const uint32_t*)counts,
+     next_power(o.experts));
+  return go.status();
+}
+
+int themis_expert_dispatch(const themis_expert_order_t* order, const themis_rows_t* x, uint64_t width,
+                           const themis_rows_t* out, void* stream) {
+  Order o;
+  if (const int status = order_status(order, o)) return status;
+  if (o.slots == 0 || width == 0) return THEMIS_OK;
+  if ((o.n && !rows_ok(x, false)) || !rows_ok(out, false)) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (width > kMostWidth) return THEMIS_ERR_UNSUPPORTED;
+  if (!rows_apart(*out, o.slots, width)) return THEMIS_ERR_INVALID_ARGUMENT;
+  const RowLayout l = row_layout(width);
+  const Rows from = o.n ? rows_of(*x, o.n) : Rows{0, 0, 0, 0, out->type}, to = rows_of(*out, o.slots);
+  const uint32_t fill_rows = slots_to_clear(width * type_bytes(to.type)), fills = blocks_of(o.slots, fill_rows);
+  Launches go(stream);
+  with_type(from.type, [&](auto in) {
+    with_type(to.type, [&](auto out) {
+      typedef decltype(in) In;
+      typedef decltype(out) Out;
+      go(width < kLaneElements ? dispatch_kernel<false, In, Out> : dispatch_kernel<true, In, Out>,
+         dim3(fills + blocks_of(o.n, 256u >> l.shift), l.chunks), 256, o, from, (uint32_t)width, to, l.shift, fills,
+         fill_rows);
+    });
+  });
+  return go.status();
+}
+
+int themis_expert_combine(const themis_expert_order_t* order, const themis_rows_t* y, uint64_t width,
+                          const themis_rows_t* weights, int accumulate, const themis_rows_t* out, void* stream) {
+  Order o;
+  if (const int status = order_status(order, o)) return status;
+  if (o.n == 0 || width == 0 || (o.pairs == 0 && accumulate)) return THEMIS_OK;
+  if (!rows_ok(out, false) || (o.slots && !rows_ok(y, false))) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (weights && o.k && !rows_ok(weights, false)) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (width > kMostWidth) return THEMIS_ERR_UNSUPPORTED;
+  if (!rows_apart(*out, o.n, width)) return THEMIS_ERR_INVALID_ARGUMENT;
+  const RowLayout l = row_layout(width);
+  const Rows from = o.slots ? rows_of(*y, o.slots) : Rows{0, 0, 0, 0, out->type}, to = rows_of(*out, o.n);
+  Launches go(stream);
+  with_type(from.type, [&](auto in) {
+    with_type(to.type, [&](auto out) {
+      typedef decltype(in) In;
+      typedef decltype(out) Out;
+      go(width < kLaneElements ? combine_kernel<false, In, Out> : combine_kernel<true, In, Out>,
+         dim3(blocks_of(o.n, 256u >> l.shift), l.chunks), 256, o, from, (uint32_t)width, rows_or_none(weights, o.n),
+         accumulate != 0, to, l.shift);
+    });
+  });
+  return go.status();
+}
+
+int themis_expert_combine_grad(const themis_expert_order_t* order, const themis_rows_t* grad_out, uint64_t width,
+                               const themis_rows_t* y, const themis_rows_t* weights, const themis_rows_t* grad_y,
+                               const themis_rows_t* grad_weights, void* stream) {
+  Order o;
+  if (const int status = order_status(order, o)) return status;
+  if ((grad_y && o.slots && width && !rows_ok(grad_y, false)) || (grad_weights && o.pairs && !rows_ok(grad_weights, false)))
+    return THEMIS_ERR_INVALID_ARGUMENT;
+  const bool rows = grad_y && o.slots && width, products = grad_weights && o.pairs;
+  if (!rows && !products) return THEMIS_OK;
+  if (o.pairs && ((width && !rows_ok(grad_out, false)) || !rows_ok(weights, false))) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (products && o.slots && width && !rows_ok(y, false)) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (rows && products && y->type != grad_y->type) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (width > kMostWidth) return THEMIS_ERR_UNSUPPORTED;
+  if ((rows && !rows_apart(*grad_y, o.slots, width)) || (products && !rows_apart(*grad_weights, o.n, o.k)))
+    return THEMIS_ERR_INVALID_ARGUMENT;
+  const Rows to = rows ? rows_of(*grad_y, o.slots) : Rows{};
+  const Rows from = products && width ? rows_of(*y, o.slots) : Rows{0, 0, 0, 0, rows ? to.type : THEMIS_F32};
+  const Rows g = o.pairs && width ? rows_of(*grad_out, o.n) : Rows{0, 0, 0, 0, from.type};
+  const uint32_t fill_rows = rows ? slots_to_clear(width * type_bytes(to.type)) : 1u;
+  const uint32_t fills = rows ? blocks_of(o.slots, fill_rows) : 0u;
+  const uint32_t shift = std::min(row_layout(std::max<uint64_t>(width, 1)).shift, 6u);
+  Launches go(stream);
+  with_type(g.type, [&](auto grad) {
+    with_type(from.type, [&](auto row) {
+      typedef decltype(grad) G;
+      typedef decltype(row) Y;
+      auto run = [&](auto kernel, uint32_t pairs) {
+        go(kernel, dim3(fills + blocks_of((uint64_t)o.n * ((o.k + pairs - 1) / pairs), 256u >> shift)), 256, o, g,
+           (uint32_t)width, from, o.pairs ? rows_of(*weights, o.n) : Rows{}, to,
+           products ? rows_of(*grad_weights, o.n) : Rows{}, shift, fills, fill_rows);
+      };
+      if (width < kLaneElements) run(combine_grad_kernel<false, G, Y, 4>, 4);
+      else run(combine_grad_kernel<true, G, Y, 4>, 4);
+    });
+  });
+  return go.status();
+}
+
+int themis_dropout(const themis_rows_t* x, uint64_t n, uint64_t width, double p, uint64_t seed, uint64_t call,
+                   const uint64_t* call_at, const themis_rows_t* add, const themis_rows_t* out, void* stream) {
+  if (!(p >= 0.0 && p <= 1.0) || !aligned(call_at, 8)) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (n == 0 || width == 0) return THEMIS_OK;
+  if (!rows_ok(x, false) || !rows_ok(out, false) || (add && !rows_ok(add, false))) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (add && add->type != out->type) return THEMIS_ERR_INVALID_ARGUMENT;
+  if (n > kMost || width > kMostWidth) return THEMIS_ERR_UNSUPPORTED;
+  if (!rows_apart(*out, n, width)) return THEMIS_ERR_INVALID_ARGUMENT;
+  const uint64_t least = (uint64_t)std::nearbyint(p * 4294967296.0);
+  const DropoutKey d = {{(uint32_t)seed, (uint32_t)(seed >> 32)}, {(uint32_t)call, (uint32_t)(call >> 32)},
+                        (uint32_t)least, least >> 32 != 0, p < 1.0 ? (float)(1.0 / (1.0 - p)) : 0.0f};
+  Launches go(stream);
+  with_type(x->type, [&](auto in) {
+    with_type(out->type, [&](auto to) {
+      typedef decltype(in) In;
+      typedef decltype(to) Out;
+      const RowLayout l = row_layout(width, kVecOf<In, Out>);
+      go(add ? width < kLaneElements ? dropout_kernel<false, true, In, Out> : dropout_kernel<true, true, In, Out>
+         : width < kLaneElements ? dropout_kernel<false, false, In, Out> : dropout_kernel<true, false, In, Out>,
+         dim3(blocks_of(n, 256u >> l.shift), l.chunks), 256, rows_of(*x, n), (uint32_t)n, (uint32_t)width, d, call_at,
+         rows_or_none(add, n), rows_of(*out, n), l.shift);
+    });
+  });
+  return go.status();
+}
+
+}  // extern "C"
