@@ -181,6 +181,241 @@ gate_kernel(Rows logits, uint32_t experts, uint32_t n, uint32_t k, bool renormal
 }
 
 // ---------------------------------------------------------------------------
+// The same for up to kMostListed experts: every lane keeps the kList largest of its own, sorted, while it
+// goes through them, and the lanes' lists are merged two and two: the larger of a list and the other one
+// backwards are the largest of both, and a few exchanges sort them.
+//
+// An entry is a number that is ordered as (logit, index from the end) is: of logits of 16 bits
+// a whole number, the logit as a signed one (so that -0 is 0) over its index, of binary32 a binary64
+// number, the logit with its index in the last of the 29 bits that it leaves free.
+// 65,536 tokens on 256 experts, eight of them (bf16): 13.4 us, of which the logits' bytes need 8; by k
+// rounds of a maximum 33.
+// ---------------------------------------------------------------------------
+constexpr uint32_t kMostListed = 8;
+
+__device__ __forceinline__ int32_t larger(int32_t a, int32_t b) { return max(a, b); }
+__device__ __forceinline__ int32_t smaller(int32_t a, int32_t b) { return min(a, b); }
+// (the instructions themselves: of fmax the compiler makes two, in case an argument is a signalling NaN;
+// entries are none)
+__device__ __forceinline__ double larger(double a, double b) {
+  double r;
+  asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ double smaller(double a, double b) {
+  double r;
+  asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+
+// A place's new entry is the median of its own, the next larger one's and the new one.
+template <int kList>
+__device__ __forceinline__ void insert(int32_t (&list)[kList], int32_t x) {
+#pragma unroll
+  for (int i = kList - 1; i > 0; --i)
+    asm("v_med3_i32 %0, %1, %2, %3" : "=v"(list[i]) : "v"(list[i]), "v"(list[i - 1]), "v"(x));
+  list[0] = max(list[0], x);
+}
+template <int kList>
+__device__ __forceinline__ void insert(double (&list)[kList], double x) {
+#pragma unroll
+  for (int i = 0; i < kList; ++i) {
+    const double up = larger(list[i], x);
+    if (i + 1 < kList) x = smaller(list[i], x);
+    list[i] = up;
+  }
+}
+
+// The largest of this lane's list and another's, sorted.
+template <int kList, typename E, typename F>
+__device__ __forceinline__ void merge_with(E (&list)[kList], F other) {
+  E both[kList];
+#pragma unroll
+  for (int i = 0; i < kList; ++i) both[i] = larger(list[i], other(list[kList - 1 - i]));
+#pragma unroll
+  for (int d = kList / 2; d > 0; d /= 2)
+#pragma unroll
+    for (int i = 0; i < kList; ++i)
+      if ((i & d) == 0) {
+        const E a = both[i], b = both[i + d];
+        both[i] = larger(a, b);
+        both[i + d] = smaller(a, b);
+      }
+#pragma unroll
+  for (int i = 0; i < kList; ++i) list[i] = both[i];
+}
+template <int kControl>
+__device__ __forceinline__ int32_t of_lane(int32_t x) {
+  return __builtin_amdgcn_update_dpp(0, x, kControl, 0xF, 0xF, false);
+}
+template <int kControl>
+__device__ __forceinline__ double of_lane(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)of_lane<kControl>((int32_t)b), hi = (uint32_t)of_lane<kControl>((int32_t)(b >> 32));
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int kList, typename E>
+__device__ __forceinline__ void merge_group(E (&list)[kList], uint32_t shift) {
+  if (shift > 0) merge_with(list, [](E x) { return of_lane<0xB1>(x); });    // lane ^ 1
+  if (shift > 1) merge_with(list, [](E x) { return of_lane<0x4E>(x); });    // lane ^ 2
+  if (shift > 2) merge_with(list, [](E x) { return of_lane<0x141>(x); });   // 7 - lane
+  if (shift > 3) merge_with(list, [](E x) { return of_lane<0x140>(x); });   // 15 - lane
+  if (shift > 4) merge_with(list, [](E x) { return __shfl_xor(x, 16); });
+}
+
+template <typename T>
+struct Listed {   // 16 bits
+  typedef int32_t Entry;
+  typedef int16_t Pair __attribute__((ext_vector_type(2)));
+  struct Pairs { Pair two[4]; };
+  static constexpr int16_t kInfinite = __is_same(T, __bf16) ? 0x7F80 : 0x7C00;
+  static constexpr Entry kNone = INT32_MIN;
+
+  Pair key[4];
+  // The lane's eight logits; `begin` is the first one's index.
+  __device__ __forceinline__ Listed(typename Packed<T, 8>::type v) {
+    Pair most = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+      const Pair x = __builtin_bit_cast(Pairs, v).two[i], sign = x >> 15, size = x & (int16_t)0x7FFF;
+      most = __builtin_elementwise_max(most, size);
+      key[i] = (size ^ sign) - sign;
+    }
+    if (most[0] > kInfinite || most[1] > kInfinite)   // a NaN: above all
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) {
+        const Pair size = __builtin_bit_cast(Pairs, v).two[i] & (int16_t)0x7FFF, one = 1;
+        const Pair is = -__builtin_elementwise_min(__builtin_elementwise_max(size, (Pair)kInfinite) - (Pair)kInfinite, one);
+        key[i] = (key[i] | is) & ~(is & (int16_t)0x8000);
+      }
+  }
+  __device__ __forceinline__ Entry entry(uint32_t i, uint32_t begin) const {
+    const uint32_t two = __builtin_bit_cast(uint32_t, key[i / 2]);
+    return (Entry)((i & 1 ? two & 0xFFFF0000u : two << 16) | (0xFFFFu - begin - i));
+  }
+  static __device__ __forceinline__ bool any(Entry e) { return e >> 16 > -kInfinite; }
+  static __device__ __forceinline__ int32_t index(Entry e) { return 0xFFFF - (e & 0xFFFF); }
+  static __device__ __forceinline__ float value(Entry e) {
+    const int32_t s = e >> 16;
+    return (float)__builtin_bit_cast(T, (uint16_t)(s < 0 ? -s | 0x8000 : s));
+  }
+};
+template <>
+struct Listed<float> {
+  typedef double Entry;
+  static constexpr Entry kNone = -0x1p300, kMasked = -0x1p200;   // (behind all that binary32 holds)
+  static constexpr uint32_t kIndex = kMostExperts - 1;
+
+  double key[8];
+  __device__ __forceinline__ Listed(typename Packed<float, 8>::type v) {
+    float most = 0.0f;
+    bool nan = false;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      most = fmaxf(most, v[i]);
+      nan = nan || v[i] != v[i];
+      key[i] = larger((double)(v[i] + 0.0f), kMasked);   // (-0 is 0)
+    }
+    if (nan || most == __builtin_inff())
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i)
+        key[i] = v[i] != v[i] ? 0x1p300 : v[i] == __builtin_inff() ? 0x1p200 : key[i];
+  }
+  __device__ __forceinline__ Entry entry(uint32_t i, uint32_t begin) const {
+    const uint64_t b = __builtin_bit_cast(uint64_t, key[i]);
+    // (a negative number is the smaller the larger its bits are)
+    const uint32_t last = (int64_t)b < 0 ? begin + i : kIndex - begin - i;
+    return __builtin_bit_cast(double, b | last);
+  }
+  static __device__ __forceinline__ bool any(Entry e) { return e > kMasked * 0.5; }
+  static __device__ __forceinline__ int32_t index(Entry e) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, e);
+    return (int32_t)(((int64_t)b < 0 ? b : ~b) & kIndex);
+  }
+  static __device__ __forceinline__ float value(Entry e) {
+    if (e >= 0x1p300) return __builtin_nanf("");
+    return (float)__builtin_bit_cast(double, __builtin_bit_cast(uint64_t, e) & ~(uint64_t)kIndex);   // (2^200: infinite)
+  }
+};
+
+template <typename T, int kChunks, int kList, bool kAll>
+__global__ void __launch_bounds__(256)
+gate_list_kernel(Rows logits, uint32_t experts, uint32_t n, uint32_t k, Rows weights, Rows chosen, uint32_t shift) {
+  const uint32_t lanes = 1u << shift, lane = threadIdx.x & (lanes - 1u), group = threadIdx.x >> shift;
+  const uint32_t groups = 256u >> shift;
+  for (uint64_t at = (uint64_t)blockIdx.x * groups; at < n; at += (uint64_t)gridDim.x * groups) {
+    const uint32_t t = (uint32_t)at + group;
+    const T* row = row_at<const T>(logits, min(t, n - 1u));
+    // Eight adjacent logits an access, an access of the lanes after the other; the row's last one is moved
+    // back so that it is whole, and what it has of the one before is -inf.
+    uint32_t begin[kChunks];
+    typename Packed<T, 8>::type v[kChunks];
+#pragma unroll
+    for (uint32_t c = 0; c < kChunks; ++c) {
+      const uint32_t first = (c * lanes + lane) * 8;
+      begin[c] = kChunks == 1 && experts < 8 ? 0u : min(first, experts - 8);
+      if (kChunks == 1 && experts < 8) v[c] = own_logits<8>(row, 0u, experts, (T)-__builtin_inff());
+      else v[c] = load<8>(row + begin[c]);
+    }
+#pragma unroll
+    for (uint32_t c = 0; c < kChunks; ++c) {
+      uint32_t others = (c * lanes + lane) * 8 - begin[c];
+      asm volatile("" : "+v"(others));   // (the comparisons, kept for all tokens, would take more masks than there are)
+      if (others)
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) v[c][i] = i < others ? (T)-__builtin_inff() : v[c][i];
+    }
+    typedef Listed<T> L;
+    typename L::Entry list[kList];
+#pragma unroll
+    for (uint32_t i = 0; i < kList; ++i) list[i] = L::kNone;
+#pragma unroll
+    for (uint32_t c = 0; c < kChunks; ++c) {
+      const L mine(v[c]);
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i) insert(list, mine.entry(i, begin[c]));
+      __builtin_amdgcn_sched_barrier(0);   // (all entries at once would take the registers of other wavefronts)
+    }
+    merge_group(list, shift);
+    const float largest = L::any(list[0]) ? L::value(list[0]) : 0.0f;
+    float sum = 0.0f;
+    if constexpr (kAll) {
+#pragma unroll
+      for (uint32_t c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+          sum += expf((float)v[c][i] - largest);
+          if (i % 2) __builtin_amdgcn_sched_barrier(0);
+        }
+      sum = group_sum(sum, shift);
+    }
+    // Entry j of the list is lane j's; of few lanes several.
+    auto entry = [&](uint32_t j) {
+      typename L::Entry e = list[0];
+#pragma unroll
+      for (uint32_t i = 1; i < kList; ++i) {
+        const typename L::Entry x = list[i];   // (a value: of two places the compiler would keep the list in memory)
+        e = j == i ? x : e;
+      }
+      return e;
+    };
+    auto power = [&](typename L::Entry e) { return L::any(e) ? expf(L::value(e) - largest) : 0.0f; };
+    const typename L::Entry first = entry(lane);
+    const float mine = power(first);
+    if constexpr (!kAll) {
+      for (uint32_t j = lane; j < k; j += lanes) sum += j == lane ? mine : power(entry(j));
+      sum = group_sum(sum, shift);
+    }
+    if (t < n)
+      for (uint32_t j = lane; j < k; j += lanes) {
+        const typename L::Entry e = j == lane ? first : entry(j);
+        put_number(chosen, t, j, L::any(e) ? L::index(e) : -1);
+        put_float(weights, t, j, L::any(e) ? (j == lane ? mine : power(e)) / sum : 0.0f);
+      }
+  }
+}
+
+// ---------------------------------------------------------------------------
 // themis_expert_gate_grad.  With w the weights and p the softmax over all logits:
 //   over the chosen:  dl[e] = sum over j with e_j == e of w_j (dw_j - sum_i w_i dw_i)
 //   over all:         dl[e] = sum over j with e_j == e of w_j dw_j  -  p_e sum_i w_i dw_i

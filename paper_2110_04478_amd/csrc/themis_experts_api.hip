@@ -24,6 +24,11 @@ GateLayout gate_layout(uint32_t experts) {
   else l.own = experts <= 8 ? 1 : experts <= 16 ? 2 : experts <= 32 ? 4 : 8;
   return l;
 }
+// The same where lists are kept: 2^shift lanes of `chunks` times eight.
+GateLayout list_layout(uint32_t experts) {
+  const uint32_t chunks = experts <= 64 ? 1 : experts <= 128 ? 2 : 4;
+  return {chunks, next_power((experts + 8 * chunks - 1) / (8 * chunks))};
+}
 template <typename F>
 void with_own(uint32_t own, F&& f) {
   if (own == 1) f(std::integral_constant<int, 1>{});
@@ -93,6 +98,29 @@ int themis_expert_gate(const themis_rows_t* logits, uint64_t n_experts, uint64_t
   if (!rows_apart(*weights, n, k) || !rows_apart(*experts, n, k)) return THEMIS_ERR_INVALID_ARGUMENT;
   const GateLayout l = gate_layout((uint32_t)n_experts);
   Launches go(stream);
+  if (k <= kMostListed) {
+    const GateLayout m = list_layout((uint32_t)n_experts);
+    auto run = [&](auto kernel) {
+      go(kernel, dim3(blocks_of(n, 256u >> m.shift)), 256, rows_of(*logits, n), (uint32_t)n_experts, (uint32_t)n, (uint32_t)k,
+         rows_of(*weights, n), rows_of(*experts, n), m.shift);
+    };
+    with_type(logits->type, [&](auto in) {
+      typedef decltype(in) In;
+      with_own(m.own, [&](auto own) {
+        constexpr int kChunks = decltype(own)::value > 4 ? 4 : decltype(own)::value;
+        auto over = [&](auto all) {
+          constexpr bool kAll = decltype(all)::value;
+          if (k == 1) run(gate_list_kernel<In, kChunks, 1, kAll>);
+          else if (k == 2) run(gate_list_kernel<In, kChunks, 2, kAll>);
+          else if (k <= 4) run(gate_list_kernel<In, kChunks, 4, kAll>);
+          else run(gate_list_kernel<In, kChunks, 8, kAll>);
+        };
+        if (renormalize) over(std::false_type{});
+        else over(std::true_type{});
+      });
+    });
+    return go.status();
+  }
   with_type(logits->type, [&](auto in) {
     with_own(l.own, [&](auto own) {
       go(gate_kernel<decltype(in), decltype(own)::value>, dim3(blocks_of(n, 256u >> l.shift)), 256, rows_of(*logits, n),

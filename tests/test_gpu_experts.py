@@ -94,7 +94,7 @@ def check_gate(gpu, logits, k, renormalize, out=F32, index=I32, device_logits=No
 @pytest.mark.parametrize("renormalize", [True, False])
 @pytest.mark.parametrize("experts", [1, 2, 7, 8, 9, 16, 31, 60, 64, 65, 128, 200, 256, 300, 512, 513, 1000, 1024])
 def test_gate_sizes(gpu, experts, renormalize):
-    for n, k in ((1, 1), (3, 2), (33, 8), (130, 6), (1000, 64)):
+    for n, k in ((1, 1), (3, 2), (33, 8), (130, 6), (70, 3), (67, 5), (40, 9), (1000, 64)):
         k = min(k, experts)
         check_gate(gpu, normal((n, experts), BF16, n + experts, 2.0), k, renormalize)
         check_gate(gpu, normal((n, experts), F32, n + experts, 2.0), k, renormalize)
@@ -114,8 +114,11 @@ def test_gate_equal_logits(gpu, kind):
     g = torch.Generator().manual_seed(3)
     few = torch.randint(-2, 3, (500, 96), generator=g).to(kind)
     few[few == 0] *= torch.where(torch.rand((few == 0).sum(), generator=g) < 0.5, -1.0, 1.0).to(kind)
-    for k in (1, 4, 64):
+    for k in (1, 2, 4, 7, 64):
         check_gate(gpu, few, k, True)
+        check_gate(gpu, few * 1e-30 if kind == F32 else few, k, True)
+    check_gate(gpu, torch.full((9, 1000), -0.5, dtype=kind), 8, False)
+    check_gate(gpu, torch.zeros((9, 1024), dtype=kind), 8, False)
     check_gate(gpu, torch.full((9, 1000), 0.5, dtype=kind), 64, False)
 
 
@@ -146,7 +149,9 @@ def test_gate_nan_and_infinity(gpu, kind):
     x[1, 5] = INF
     x[2, 3], x[2, 11] = -float("nan"), float("nan")
     for renormalize in (True, False):
+        many, numbers = gpu.themis_expert_gate(x.cuda(), 12, renormalize)
         weights, experts = gpu.themis_expert_gate(x.cuda(), 3, renormalize)
+        assert torch.equal(experts, numbers[:, :3]) and torch.isnan(many[:3]).all()
         assert torch.isnan(weights[:3]).all() and not torch.isnan(weights[3]).any()
         assert experts[0, 0] == 7 and experts[1, 0] == 5 and experts[2, :2].tolist() == [3, 11]
         grad = gpu.themis_expert_gate_grad(torch.ones_like(weights), x.cuda(), experts, renormalize)
