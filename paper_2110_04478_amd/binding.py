@@ -800,6 +800,11 @@ class ExpertOrder:
         return stream
 
 
+@functools.lru_cache(maxsize=1024)
+def themis_expert_sort_workspace_bytes(n: int, k: int, n_experts: int) -> int:
+    return lib().themis_expert_sort_workspace_bytes(n, k, n_experts)
+
+
 def themis_expert_sort(experts: torch.Tensor, n_experts: int, capacity: int = 0,
                        workspace: Optional[torch.Tensor] = None) -> ExpertOrder:
     """Orders the pairs of experts [.., k] by expert, an expert's in the tokens' order.
@@ -815,17 +820,16 @@ def themis_expert_sort(experts: torch.Tensor, n_experts: int, capacity: int = 0,
     slots = n_experts * capacity if capacity else pairs
     if max(n, k, pairs, slots, n_experts) >= 1 << 31:
         raise ThemisError(UNSUPPORTED)
-    new = functools.partial(torch.empty, dtype=torch.int32, device=experts.device)
-    order = _ExpertOrder(n, k, n_experts, capacity)
-    # (one allocation for all four: a call on a few tokens is the host's time)
-    place, counts, starts, source = torch.split_with_sizes(new(pairs + 2 * n_experts + 1 + slots),
-                                                           (pairs, n_experts, n_experts + 1, slots))
-    order.place, order.counts, order.starts, order.source = (t.data_ptr() for t in (place, counts, starts, source))
-    need = lib().themis_expert_sort_workspace_bytes(n, k, n_experts)
-    if workspace is None and need:
-        workspace = alloc_workspace(need, experts.device)
-    at, size = (None, 0) if workspace is None else (workspace.data_ptr(),
-                                                    workspace.numel() * workspace.element_size())
+    # (one allocation for all of it, the workspace too: a call on a few tokens is the host's time)
+    own = 0 if workspace is not None else (themis_expert_sort_workspace_bytes(n, k, n_experts) + 15) // 16 * 4
+    room = torch.empty(own + pairs + 2 * n_experts + 1 + slots, dtype=torch.int32, device=experts.device)
+    first = room.data_ptr()
+    at, size = (first, 4 * own) if workspace is None else (workspace.data_ptr(),
+                                                           workspace.numel() * workspace.element_size())
+    _, place, counts, starts, source = torch.split_with_sizes(room, (own, pairs, n_experts, n_experts + 1, slots))
+    first += 4 * own
+    order = _ExpertOrder(n, k, n_experts, capacity, first, first + 4 * pairs, first + 4 * (pairs + n_experts),
+                         first + 4 * (pairs + 2 * n_experts + 1))
     rows_e, experts = _read_rows(experts, experts.dim() - 1, k)
     _check(lib().themis_expert_sort(rows_e, order, at, size, stream))
     return ExpertOrder(place.view(experts.shape), counts, starts, source, capacity, order, {stream})

@@ -557,7 +557,7 @@ expert_count_kernel(Order o, Rows chosen, uint32_t part, uint32_t* counts) {
 __global__ void __launch_bounds__(kPairGroup)
 expert_sort_kernel(Order o, Rows chosen, uint32_t part, uint32_t parts, const uint32_t* counts, uint32_t bits) {
   __shared__ uint32_t next[kPairWaves][kMostExperts];   // first a wavefront's counts, then where its next one goes
-  __shared__ uint32_t wave_sums[kPairWaves];
+  __shared__ uint32_t wave_sums[kPairWaves], shared_before[kPairGroup], shared_all[kPairGroup];
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
   const uint32_t first = blockIdx.x * part, share = part / kPairWaves;   // (a multiple of 64)
   const uint32_t begin = min(first + wave * share, o.pairs), end = min(begin + share, o.pairs);
@@ -565,28 +565,49 @@ expert_sort_kernel(Order o, Rows chosen, uint32_t part, uint32_t parts, const ui
   if (b < o.experts)
 #pragma unroll
     for (uint32_t w = 0; w < kPairWaves; ++w) next[w][b] = 0;
+  uint32_t expert[kPairsAhead];   // (of the first turn: read before the barrier, and kept where it is the only one)
+  {
+    uint32_t at[kPairsAhead];
+#pragma unroll
+    for (uint32_t k = 0; k < kPairsAhead; ++k) at[k] = min(begin + k * 64 + lane, o.pairs - 1u);
+    if (begin < end) experts_of(o, chosen, at, expert);
+  }
   __syncthreads();
   for (uint32_t i = begin; i < end; i += kPairsAhead * 64) {
-    uint32_t at[kPairsAhead], expert[kPairsAhead];
+    uint32_t at[kPairsAhead];
 #pragma unroll
     for (uint32_t k = 0; k < kPairsAhead; ++k) at[k] = min(i + k * 64 + lane, end - 1u);
-    experts_of(o, chosen, at, expert);
+    if (i != begin) experts_of(o, chosen, at, expert);
 #pragma unroll
     for (uint32_t k = 0; k < kPairsAhead; ++k)
       count_expert(next[wave], expert[k], i + k * 64 + lane < end && expert[k] != ~0u);
   }
-  uint32_t before = 0, all = 0;   // of this lane's expert: in the parts before, in all
-  if (parts > 1 && b < o.experts) {
-    for (uint32_t p = 0; p < parts; p += kPartsAhead) {
-      uint32_t c[kPartsAhead];
+  // Of every expert: pairs in the parts before, and in all.  The lanes of an expert take some parts each.
+  uint32_t before = 0, all = 0;
+  if (parts > 1) {
+    const uint32_t e = threadIdx.x & ((1u << bits) - 1u), sharer = threadIdx.x >> bits;
+    const uint32_t some = max((parts + (kPairGroup >> bits) - 1) / (kPairGroup >> bits), kPartsAhead);
+    const uint32_t sharers = (parts + some - 1) / some, from = min(sharer * some, parts), to = min(from + some, parts);
+    if (e < o.experts)
+      for (uint32_t p = from; p < to; p += kPartsAhead) {
+        uint32_t c[kPartsAhead];
 #pragma unroll
-      for (uint32_t k = 0; k < kPartsAhead; ++k) c[k] = counts[min(p + k, parts - 1u) * o.experts + b];
+        for (uint32_t k = 0; k < kPartsAhead; ++k) c[k] = counts[min(p + k, to - 1u) * o.experts + e];
 #pragma unroll
-      for (uint32_t k = 0; k < kPartsAhead; ++k) {
-        before += p + k < blockIdx.x ? c[k] : 0u;
-        all += p + k < parts ? c[k] : 0u;
+        for (uint32_t k = 0; k < kPartsAhead; ++k) {
+          before += p + k < min(to, blockIdx.x) ? c[k] : 0u;
+          all += p + k < to ? c[k] : 0u;
+        }
       }
-    }
+    shared_before[threadIdx.x] = before;
+    shared_all[threadIdx.x] = all;
+    __syncthreads();
+    before = all = 0;
+    if (b < o.experts)
+      for (uint32_t q = 0; q < sharers; ++q) {
+        before += shared_before[(q << bits) + b];
+        all += shared_all[(q << bits) + b];
+      }
   }
   __syncthreads();   // (the wavefronts' counts are complete)
   if (parts == 1 && b < o.experts)
@@ -616,8 +637,12 @@ expert_sort_kernel(Order o, Rows chosen, uint32_t part, uint32_t parts, const ui
       at += c;
     }
   }
-  __shared__ uint32_t starts[kMostExperts];
-  if (b < o.experts) starts[b] = start;
+  uint32_t* starts = shared_before;   // (read above for the last time before the last barrier)
+  uint32_t* filled = shared_all;
+  if (b < o.experts) {
+    starts[b] = start;
+    filled[b] = all;
+  }
   if (blockIdx.x == 0) {
     if (b < o.experts) {
       o.counts[b] = (int32_t)all;
@@ -627,10 +652,10 @@ expert_sort_kernel(Order o, Rows chosen, uint32_t part, uint32_t parts, const ui
   }
   __syncthreads();
   for (uint32_t i0 = begin; i0 < end; i0 += kPairsAhead * 64) {
-    uint32_t from[kPairsAhead], expert[kPairsAhead];
+    uint32_t from[kPairsAhead];
 #pragma unroll
     for (uint32_t k = 0; k < kPairsAhead; ++k) from[k] = min(i0 + k * 64 + lane, end - 1u);
-    experts_of(o, chosen, from, expert);
+    if (share > kPairsAhead * 64) experts_of(o, chosen, from, expert);
 #pragma unroll
     for (uint32_t k = 0; k < kPairsAhead; ++k) {
       if (i0 + k * 64 >= end) break;
@@ -659,9 +684,6 @@ expert_sort_kernel(Order o, Rows chosen, uint32_t part, uint32_t parts, const ui
       o.source[s] = -1;
     return;
   }
-  __shared__ uint32_t filled[kMostExperts];
-  if (b < o.experts) filled[b] = all;
-  __syncthreads();
   for (uint64_t e = blockIdx.x * kPairWaves + wave; e < o.experts; e += (uint64_t)parts * kPairWaves)
     for (uint64_t s = (uint64_t)filled[e] + lane; s < o.capacity; s += 64) o.source[e * o.capacity + s] = -1;
 }
