@@ -86,9 +86,9 @@ struct Access {
     at = width >= kLaneElements ? min(first, width - kVec) : first;
     skip = count ? first - at : 0u;
   }
-  template <bool kWhole, typename T>
+  template <bool kWhole, bool kOnce = false, typename T>
   __device__ __forceinline__ typename Packed<T, kVec>::type read(const T* row) const {
-    return kWhole ? load<kVec>(row + at) : load_some<kVec>(row + at, count);
+    return !kWhole ? load_some<kVec>(row + at, count) : kOnce ? load_once<kVec>(row + at) : load<kVec>(row + at);
   }
   template <bool kWhole, typename T>
   __device__ __forceinline__ void write(T* row, Floats<kVec> v) const {
@@ -130,8 +130,8 @@ struct Slice<8> {
   Access<8> a;
   __device__ __forceinline__ Slice(uint32_t first, uint32_t lane, uint32_t, uint32_t width) : a(first + lane * 8, width) {}
   __device__ __forceinline__ bool any() const { return a.count != 0; }
-  template <bool kWhole, typename T>
-  __device__ __forceinline__ typename Packed<T, 8>::type read(const T* row) const { return a.read<kWhole>(row); }
+  template <bool kWhole, bool kOnce = false, typename T>
+  __device__ __forceinline__ typename Packed<T, 8>::type read(const T* row) const { return a.read<kWhole, kOnce>(row); }
   template <bool kWhole, typename T>
   __device__ __forceinline__ void write(T* row, float8 v) const { a.write<kWhole>(row, v); }
   template <bool kWhole>
@@ -145,9 +145,9 @@ struct Slice<4> {
   __device__ __forceinline__ Slice(uint32_t first, uint32_t lane, uint32_t lanes, uint32_t width)
       : a(first + lane * 4, width), b(first + (lanes + lane) * 4, width) {}
   __device__ __forceinline__ bool any() const { return a.count != 0; }
-  template <bool kWhole, typename T>
+  template <bool kWhole, bool kOnce = false, typename T>
   __device__ __forceinline__ typename Packed<T, 8>::type read(const T* row) const {
-    return __builtin_shufflevector(a.read<kWhole>(row), b.read<kWhole>(row), 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_shufflevector(a.read<kWhole, kOnce>(row), b.read<kWhole, kOnce>(row), 0, 1, 2, 3, 4, 5, 6, 7);
   }
   template <bool kWhole, typename T>
   __device__ __forceinline__ void write(T* row, float8 v) const {

@@ -707,16 +707,19 @@ __device__ __forceinline__ void clear_empty_slots(const Order& o, uint32_t block
 }
 
 // themis_expert_dispatch: a row is read once and written to its token's slots; the first `fills`
-// workgroups clear the slots of no pair.
+// workgroups clear the slots of no pair, the others take the chunks of a row side by side.
 template <bool kWhole, typename In, typename Out>
 __global__ void __launch_bounds__(256)
-dispatch_kernel(Order o, Rows x, uint32_t width, Rows out, uint32_t shift, uint32_t fills, uint32_t fill_rows) {
+dispatch_kernel(Order o, Rows x, uint32_t width, Rows out, uint32_t shift, uint32_t chunks, uint32_t fills,
+                uint32_t fill_rows) {
   if (blockIdx.x < fills) {
-    if (blockIdx.y == 0) clear_empty_slots<kWhole, Out>(o, blockIdx.x, fills, fill_rows, width, out);
+    clear_empty_slots<kWhole, Out>(o, blockIdx.x, fills, fill_rows, width, out);
     return;
   }
-  const uint32_t lanes = 1u << shift, groups = 256u >> shift, block = blockIdx.x - fills, blocks = gridDim.x - fills;
-  const Slice<kVecOf<In, Out>> slice(blockIdx.y * 256u * kLaneElements, threadIdx.x & (lanes - 1u), lanes, width);
+  const uint32_t lanes = 1u << shift, groups = 256u >> shift;
+  const uint32_t block = (blockIdx.x - fills) / chunks, chunk = (blockIdx.x - fills) % chunks;
+  const uint32_t blocks = (gridDim.x - fills) / chunks;
+  const Slice<kVecOf<In, Out>> slice(chunk * 256u * kLaneElements, threadIdx.x & (lanes - 1u), lanes, width);
   if (!slice.any()) return;
   for (uint64_t t = (uint64_t)block * groups + (threadIdx.x >> shift); t < o.n; t += (uint64_t)blocks * groups) {
     const int32_t* place = o.place + t * o.k;
@@ -730,13 +733,14 @@ dispatch_kernel(Order o, Rows x, uint32_t width, Rows out, uint32_t shift, uint3
 
 // themis_expert_combine: out[t] (+)= sum over j of weights[t][j] * y[place[t][j]], kAhead rows in flight.
 constexpr uint32_t kCombineAhead = 4;
-template <bool kWhole, typename In, typename Out>
+template <bool kWhole, bool kOnce, typename In, typename Out>
 __global__ void __launch_bounds__(256)
-combine_kernel(Order o, Rows y, uint32_t width, Rows weights, bool accumulate, Rows out, uint32_t shift) {
+combine_kernel(Order o, Rows y, uint32_t width, Rows weights, bool accumulate, Rows out, uint32_t shift, uint32_t chunks) {
   const uint32_t lanes = 1u << shift, groups = 256u >> shift;
-  const Slice<kVecOf<In, Out>> slice(blockIdx.y * 256u * kLaneElements, threadIdx.x & (lanes - 1u), lanes, width);
+  const uint32_t block = blockIdx.x / chunks, chunk = blockIdx.x % chunks, blocks = gridDim.x / chunks;
+  const Slice<kVecOf<In, Out>> slice(chunk * 256u * kLaneElements, threadIdx.x & (lanes - 1u), lanes, width);
   if (!slice.any()) return;
-  for (uint64_t t = (uint64_t)blockIdx.x * groups + (threadIdx.x >> shift); t < o.n; t += (uint64_t)gridDim.x * groups) {
+  for (uint64_t t = (uint64_t)block * groups + (threadIdx.x >> shift); t < o.n; t += (uint64_t)blocks * groups) {
     const int32_t* place = o.place + t * o.k;
     float8 sum = 0.0f;
     for (uint32_t j0 = 0; j0 < o.k; j0 += kCombineAhead) {
@@ -752,7 +756,7 @@ combine_kernel(Order o, Rows y, uint32_t width, Rows weights, bool accumulate, R
 #pragma unroll
       for (uint32_t u = 0; u < kCombineAhead; ++u) {
         v[u] = {};
-        if (s[u] < o.slots) v[u] = slice.template read<kWhole>(row_at<const In>(y, s[u]));
+        if (s[u] < o.slots) v[u] = slice.template read<kWhole, kOnce>(row_at<const In>(y, s[u]));
       }
 #pragma unroll
       for (uint32_t u = 0; u < kCombineAhead; ++u)
@@ -767,7 +771,7 @@ combine_kernel(Order o, Rows y, uint32_t width, Rows weights, bool accumulate, R
 // themis_expert_combine_grad: rows[s] = weights[a] * grad[t] and weights'[a] = <grad[t], y[s]> for the pair
 // a = (t, j) in slot s.  2^shift lanes (up to a wavefront) take kPairs of a token's pairs over the whole
 // row, so that a product is summed where it is made.
-template <bool kWhole, typename G, typename Y, int kPairs>
+template <bool kWhole, bool kOnce, typename G, typename Y, int kPairs>
 __global__ void __launch_bounds__(256)
 combine_grad_kernel(Order o, Rows grad, uint32_t width, Rows y, Rows weights, Rows rows, Rows grad_weights, uint32_t shift,
                     uint32_t fills, uint32_t fill_rows) {
@@ -799,7 +803,7 @@ combine_grad_kernel(Order o, Rows grad, uint32_t width, Rows y, Rows weights, Ro
 #pragma unroll
       for (uint32_t u = 0; u < kPairs; ++u) {
         v[u] = {};
-        if (grad_weights.data && s[u] < o.slots) v[u] = slice.template read<kWhole>(row_at<const Y>(y, s[u]));
+        if (grad_weights.data && s[u] < o.slots) v[u] = slice.template read<kWhole, kOnce>(row_at<const Y>(y, s[u]));
       }
 #pragma unroll
       for (uint32_t u = 0; u < kPairs; ++u) {

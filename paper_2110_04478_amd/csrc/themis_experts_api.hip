@@ -82,6 +82,18 @@ RowLayout row_layout(uint64_t width, uint32_t vec = kLaneElements) {
   return {std::min(next_power(vecs), 8u), (vecs + 255) / 256};
 }
 
+// Workgroups where a row's chunks are side by side.  (8 KiB rows into the order: 217 us, one chunk of all rows
+// after the other 221.)
+uint32_t chunk_blocks(uint64_t n, RowLayout l) {
+  return l.chunks * (uint32_t)std::min<uint64_t>((n + (256u >> l.shift) - 1) / (256u >> l.shift), std::max(1u, (1u << 22) / l.chunks));
+}
+
+// Rows of experts that the last cache level cannot hold are read past it (1.07 GB: sums 229 us, through it
+// 255; 335 MB: gradients 115, 138); the others may still be there (200 MB: 28 us, 24).
+bool read_once(const Order& o, uint64_t width, int type) {
+  return (uint64_t)std::min(o.slots, o.pairs) * width * type_bytes(type) >= 256u << 20;
+}
+
 // Slots of a workgroup that looks for those of no pair: about 256 KiB.
 uint32_t slots_to_clear(uint64_t row_bytes) {
   return (uint32_t)std::min<uint64_t>(64, std::max<uint64_t>(1, (256u << 10) / row_bytes));
@@ -200,8 +212,7 @@ int themis_expert_dispatch(const themis_expert_order_t* order, const themis_rows
       typedef decltype(in) In;
       typedef decltype(out) Out;
       go(width < kLaneElements ? dispatch_kernel<false, In, Out> : dispatch_kernel<true, In, Out>,
-         dim3(fills + blocks_of(o.n, 256u >> l.shift), l.chunks), 256, o, from, (uint32_t)width, to, l.shift, fills,
-         fill_rows);
+         dim3(fills + chunk_blocks(o.n, l)), 256, o, from, (uint32_t)width, to, l.shift, l.chunks, fills, fill_rows);
     });
   });
   return go.status();
@@ -218,14 +229,17 @@ int themis_expert_combine(const themis_expert_order_t* order, const themis_rows_
   if (!rows_apart(*out, o.n, width)) return THEMIS_ERR_INVALID_ARGUMENT;
   const RowLayout l = row_layout(width);
   const Rows from = o.slots ? rows_of(*y, o.slots) : Rows{0, 0, 0, 0, out->type}, to = rows_of(*out, o.n);
+  const bool once = read_once(o, width, from.type);
   Launches go(stream);
   with_type(from.type, [&](auto in) {
     with_type(to.type, [&](auto out) {
       typedef decltype(in) In;
       typedef decltype(out) Out;
-      go(width < kLaneElements ? combine_kernel<false, In, Out> : combine_kernel<true, In, Out>,
-         dim3(blocks_of(o.n, 256u >> l.shift), l.chunks), 256, o, from, (uint32_t)width, rows_or_none(weights, o.n),
-         accumulate != 0, to, l.shift);
+      go(width < kLaneElements ? combine_kernel<false, false, In, Out>
+         : once                ? combine_kernel<true, true, In, Out>
+                               : combine_kernel<true, false, In, Out>,
+         dim3(chunk_blocks(o.n, l)), 256, o, from, (uint32_t)width, rows_or_none(weights, o.n), accumulate != 0, to, l.shift,
+         l.chunks);
     });
   });
   return go.status();
@@ -252,6 +266,7 @@ int themis_expert_combine_grad(const themis_expert_order_t* order, const themis_
   const uint32_t fill_rows = rows ? slots_to_clear(width * type_bytes(to.type)) : 1u;
   const uint32_t fills = rows ? blocks_of(o.slots, fill_rows) : 0u;
   const uint32_t shift = std::min(row_layout(std::max<uint64_t>(width, 1)).shift, 6u);
+  const bool once = read_once(o, width, from.type);
   Launches go(stream);
   with_type(g.type, [&](auto grad) {
     with_type(from.type, [&](auto row) {
@@ -262,8 +277,11 @@ int themis_expert_combine_grad(const themis_expert_order_t* order, const themis_
            (uint32_t)width, from, o.pairs ? rows_of(*weights, o.n) : Rows{}, to,
            products ? rows_of(*grad_weights, o.n) : Rows{}, shift, fills, fill_rows);
       };
-      if (width < kLaneElements) run(combine_grad_kernel<false, G, Y, 4>, 4);
-      else run(combine_grad_kernel<true, G, Y, 4>, 4);
+      // Four pairs of a token where a wavefront has their rows in one turn (65,536 tokens of 512, k = 8: 229 us,
+      // with two 257), two of longer rows, for more wavefronts (16,384 of 2,048: 214, with four 224).
+      if (width < kLaneElements) run(combine_grad_kernel<false, false, G, Y, 2>, 2);
+      else if (width <= 512 && o.k > 2) run(once ? combine_grad_kernel<true, true, G, Y, 4> : combine_grad_kernel<true, false, G, Y, 4>, 4);
+      else run(once ? combine_grad_kernel<true, true, G, Y, 2> : combine_grad_kernel<true, false, G, Y, 2>, 2);
     });
   });
   return go.status();
