@@ -23,9 +23,10 @@ __device__ __forceinline__ void philox(const DropoutKey& d, uint32_t block, uint
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    // (0x96: exclusive or of three, which the compiler makes two instructions)
+    c0 = __builtin_amdgcn_bitop3_b32((uint32_t)(b >> 32), c1, k0, 0x96);
     c1 = (uint32_t)b;
-    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c2 = __builtin_amdgcn_bitop3_b32((uint32_t)(a >> 32), c3, k1, 0x96);
     c3 = (uint32_t)a;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
@@ -50,29 +51,40 @@ __device__ __forceinline__ Floats<kVec> drop(const DropoutKey& d, const Access<k
   return x;
 }
 
-// 2^shift lanes take a row (a chunk of 256 accesses of a longer one: blockIdx.y).
-template <bool kWhole, bool kAdd, typename In, typename Out>
+// 2^shift lanes take a row (one of its `chunks` of 256 accesses, side by side), kRows rows a lane. kOnce:
+// past the caches.
+template <bool kWhole, bool kOnce, bool kAdd, int kRows, typename In, typename Out>
 __global__ void __launch_bounds__(256)
 dropout_kernel(Rows x, uint32_t n, uint32_t width, DropoutKey d, const uint64_t* call_at, Rows add, Rows out,
-               uint32_t shift) {
+               uint32_t shift, uint32_t chunks) {
   constexpr int kVec = kVecOf<In, Out>;
   const uint32_t lanes = 1u << shift, groups = 256u >> shift;
-  const Access<kVec> a((blockIdx.y * 256u + (threadIdx.x & (lanes - 1u))) * kVec, width);
+  const uint32_t block = blockIdx.x / chunks, chunk = blockIdx.x % chunks, step = gridDim.x / chunks * groups * kRows;
+  const Access<kVec> a((chunk * 256u + (threadIdx.x & (lanes - 1u))) * kVec, width);
   if (!a.count) return;
   if (call_at) {
     const uint64_t call = ((uint64_t)d.call[1] << 32 | d.call[0]) + *call_at;
     d.call[0] = (uint32_t)call;
     d.call[1] = (uint32_t)(call >> 32);
   }
-  for (uint64_t r = (uint64_t)blockIdx.x * groups + (threadIdx.x >> shift); r < n; r += (uint64_t)gridDim.x * groups) {
-    const uint32_t row = (uint32_t)r;
-    Out* to = row_at<Out>(out, row);
-    const auto v = a.template read<kWhole>(row_at<const In>(x, row));
-    Floats<kVec> held = 0.0f;
-    if constexpr (kAdd) held = widen<kVec>(a.template read<kWhole>(row_at<const Out>(add, row)));
-    Floats<kVec> kept = drop<kVec>(d, a, row, widen<kVec>(v));
-    if constexpr (kAdd) kept += held;
-    a.template write<kWhole>(to, kept);
+  for (uint64_t first = (uint64_t)block * groups * kRows + (threadIdx.x >> shift); first < n; first += step) {
+    typename Packed<In, kVec>::type v[kRows];
+    typename Packed<Out, kVec>::type held[kRows];
+#pragma unroll
+    for (uint32_t u = 0; u < kRows; ++u) {
+      const uint32_t row = min((uint32_t)first + u * groups, n - 1u);
+      v[u] = a.template read<kWhole, kOnce>(row_at<const In>(x, row));
+      if constexpr (kAdd) held[u] = a.template read<kWhole, kOnce>(row_at<const Out>(add, row));
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < kRows; ++u) {
+      const uint32_t row = (uint32_t)first + u * groups;
+      if (row >= n) break;
+      Floats<kVec> kept = drop<kVec>(d, a, row, widen<kVec>(v[u]));
+      if constexpr (kAdd) kept += widen<kVec>(held[u]);
+      // (its own elements and no others: x or add may be where out is)
+      a.template write<kWhole, kOnce>(row_at<Out>(out, row), kept);
+    }
   }
 }
 

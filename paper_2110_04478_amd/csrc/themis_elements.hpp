@@ -90,10 +90,10 @@ struct Access {
   __device__ __forceinline__ typename Packed<T, kVec>::type read(const T* row) const {
     return !kWhole ? load_some<kVec>(row + at, count) : kOnce ? load_once<kVec>(row + at) : load<kVec>(row + at);
   }
-  template <bool kWhole, typename T>
+  template <bool kWhole, bool kAway = false, typename T>
   __device__ __forceinline__ void write(T* row, Floats<kVec> v) const {
     if (!kWhole) return store_some<kVec>(row + at, v, count);
-    if (count == kVec) return store<kVec>(row + at, v);
+    if (count == kVec) return kAway ? store_away<kVec>(row + at, v) : store<kVec>(row + at, v);
     if (!count) return;
 #pragma unroll
     for (uint32_t k = 1; k < kVec; ++k)

@@ -148,6 +148,25 @@ def test_in_place(gpu, width):
     same(d, dropout_of(x, 0.3, 1, 2, x, BF16))
 
 
+@pytest.mark.parametrize("kind,width,n", [(BF16, 4096, 20000), (F16, 1001, 70001), (F32, 2055, 20001)])
+def test_more_than_the_last_cache_level_holds(gpu, kind, width, n):
+    """Another kernel there: the first rows as a small call gives them, the last ones by the definition."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(n, width, generator=g, device="cuda").to(kind)
+    held = torch.randn(n, width, generator=g, device="cuda").to(kind)
+    assert x.numel() * x.element_size() * 2 >= 1 << 28
+    kept = torch.from_numpy(kept_of(n, width, 0.3, 3, 4)[-200:])
+    for add in (None, held):
+        got = gpu.themis_dropout(x, 0.3, 3, 4, add=add)
+        few = gpu.themis_dropout(x[:1000], 0.3, 3, 4, add=None if add is None else add[:1000])
+        same(got[:1000], few)
+        last = torch.where(kept, x[-200:].cpu().float() * float(np.float32(1 / (1 - 0.3))), 0.0)
+        same(got[-200:], (last if add is None else last + add[-200:].cpu().float()).to(kind))
+        out = x.clone() if add is None else add.clone()
+        gpu.themis_dropout(out if add is None else x, 0.3, 3, 4, add=None if add is None else out, out=out)
+        same(out, got)
+
+
 def test_nothing(gpu):
     assert gpu.themis_dropout(torch.ones(0, 5).cuda(), 0.3, 1, 2).shape == (0, 5)
     assert gpu.themis_dropout(torch.ones(5, 0).cuda(), 0.3, 1, 2).shape == (5, 0)

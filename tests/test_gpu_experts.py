@@ -501,6 +501,48 @@ def test_an_order_that_is_none_is_not_followed(gpu):
     assert products[3, 0] == 0 and products[4, 1] == 0
 
 
+@pytest.mark.parametrize("kind,width,k,capacity", [(BF16, 4096, 3, 0), (F32, 1030, 2, 9000), (F16, 500, 8, 0)])
+def test_rows_beyond_the_last_cache_level(gpu, kind, width, k, capacity):
+    """Read another way there: the same as in two calls on half of the columns, which are not; products
+    of the halves add up (two sums of width / 2 terms in binary32, one addition)."""
+    n = (1 << 28) // (width * k * kind.itemsize) + 5
+    g = torch.Generator(device="cuda").manual_seed(2)
+    chosen = torch.randint(0, 8, (n, k), generator=g, device="cuda", dtype=I32)
+    order = gpu.themis_expert_sort(chosen, 8, n * k // 8 + 100 if capacity else 0)
+    make = lambda *shape: torch.randn(shape, generator=g, device="cuda")   # noqa: E731
+    y, w, grad = make(order.slots, width).to(kind), make(n, k), make(n, width).to(BF16)
+    whole, (rows, products) = gpu.themis_expert_combine(y, order, w), gpu.themis_expert_combine_grad(grad, y, order, w)
+    half, sums = width // 2, []
+    for c in (slice(0, half), slice(half, width)):
+        same(gpu.themis_expert_combine(y[:, c], order, w), whole[:, c])
+        part, product = gpu.themis_expert_combine_grad(grad[:, c], y[:, c], order, w)
+        same(part, rows[:, c])
+        sums.append(product.double())
+    at = order.place.long().clamp(min=0)
+    size = torch.stack([(grad.double() * y[at[:, j]].double()).abs().sum(1) for j in range(k)], 1)
+    assert bool(((products.double() - sum(sums)).abs() <= (width + 4) * U * size + 2.0 ** -149).all())
+
+
+def test_places_beyond_32_bits(gpu):
+    """4.5 G elements in the order and back."""
+    n, k, width = 140000, 8, 4096
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((n, width), generator=g, device="cuda").to(BF16)
+    order = gpu.themis_expert_sort(torch.randint(0, 16, (n, k), generator=g, device="cuda", dtype=I32), 16)
+    rows = gpu.themis_expert_dispatch(x, order)
+    assert rows.numel() > 1 << 32
+    for s in range(0, order.slots, 1 << 17):
+        assert torch.equal(rows[s:s + (1 << 17)], x[(order.source[s:s + (1 << 17)] // k).long()])
+    # eight equal rows times weights of a power of two: exact
+    w = torch.full((n, k), 0.125, device="cuda")
+    assert torch.equal(gpu.themis_expert_combine(rows, order, w), x)
+    back, products = gpu.themis_expert_combine_grad(x, rows, order, w)
+    for s in range(0, order.slots, 1 << 17):
+        assert torch.equal(back[s:s + (1 << 17)], rows[s:s + (1 << 17)] * 0.125)
+    norms = x.double().square().sum(1, keepdim=True)
+    assert bool(((products.double() - norms).abs() <= (width + 3) * U * norms).all())
+
+
 def test_equal_calls_give_equal_bits(gpu):
     order, _ = an_order(gpu, (3000, 4), 16, 600, 1)
     y, w, g = normal((9600, 1000), BF16, 1).cuda(), normal((3000, 4), F32, 2).cuda(), normal((3000, 1000), F32, 3).cuda()
