@@ -724,6 +724,11 @@ def _written_rows(t: torch.Tensor, width: int) -> _Rows:
     return r
 
 
+def _new_rows(t: torch.Tensor, width: int) -> _Rows:
+    """The same of a tensor that this call has made."""
+    return _Rows(t.data_ptr(), _TYPES[t.dtype], 1 << 31, 0, width)
+
+
 def themis_expert_gate(logits: torch.Tensor, k: int, renormalize: bool = True,
                        out_dtype: torch.dtype = torch.float32, index_dtype: torch.dtype = torch.int32) -> tuple:
     """The k largest of the last dimension, equal ones in ascending order -> (weights [.., k]: their
@@ -742,8 +747,8 @@ def themis_expert_gate(logits: torch.Tensor, k: int, renormalize: bool = True,
     stream = _stream_here(device)
     n = weights.numel() // k
     rows_l, logits = _read_rows(logits, len(shape) - 1, n_experts)
-    _check(lib().themis_expert_gate(rows_l, n_experts, n, k, int(renormalize), _written_rows(weights, k),
-                                    _written_rows(experts, k), stream))
+    _check(lib().themis_expert_gate(rows_l, n_experts, n, k, int(renormalize), _new_rows(weights, k),
+                                    _new_rows(experts, k), stream))
     return weights, experts
 
 
@@ -757,7 +762,7 @@ def themis_expert_gate_grad(grad_weights: torch.Tensor, logits: torch.Tensor, ex
           experts.shape[:-1] == logits.shape[:-1] and grad_weights.shape == experts.shape and
           grad_weights.get_device() == device and experts.get_device() == device and
           out_dtype in (None, *_FLOATS))
-    grad = torch.empty(logits.shape, dtype=out_dtype or logits.dtype, device=logits.device)
+    grad = logits.new_empty(logits.shape, dtype=out_dtype)
     if grad.numel() == 0:
         return grad
     stream = _stream_here(device)
@@ -766,7 +771,7 @@ def themis_expert_gate_grad(grad_weights: torch.Tensor, logits: torch.Tensor, ex
     rows_l, logits = _read_rows(logits, lead, n_experts)
     rows_e, experts = _read_rows(experts, lead, k)
     _check(lib().themis_expert_gate_grad(rows_g, rows_l, n_experts, rows_e, grad.numel() // n_experts, k,
-                                         int(renormalize), _written_rows(grad, n_experts), stream))
+                                         int(renormalize), _new_rows(grad, n_experts), stream))
     return grad
 
 
@@ -778,21 +783,16 @@ class ExpertOrder:
     starts: torch.Tensor   # i32 [n_experts + 1]: first slot of an expert; behind the last
     source: torch.Tensor   # i32 [slots]: the pair of a slot, token * k + j, -1 for none
     capacity: int          # slots of an expert; 0: packed
+    slots: int
+    shape: torch.Size      # of the tokens
+    pairs: torch.Size      # of place
+    device: int
     c_struct: _ExpertOrder
     streams: set           # raw handles: the one it was made on, and others that have used it
 
-    @property
-    def shape(self):
-        """Of the tokens."""
-        return self.place.shape[:-1]
-
-    @property
-    def slots(self) -> int:
-        return self.source.shape[0]
-
     def stream(self) -> int:
         """The current stream; the order's memory, once it is given up, waits for it."""
-        stream = _stream_here(self.place.get_device())
+        stream = _stream_here(self.device)
         if stream not in self.streams:
             self.streams.add(stream)
             for t in (self.place, self.counts, self.starts, self.source):
@@ -830,15 +830,28 @@ def themis_expert_sort(experts: torch.Tensor, n_experts: int, capacity: int = 0,
     first += 4 * own
     order = _ExpertOrder(n, k, n_experts, capacity, first, first + 4 * pairs, first + 4 * (pairs + n_experts),
                          first + 4 * (pairs + 2 * n_experts + 1))
-    rows_e, experts = _read_rows(experts, experts.dim() - 1, k)
+    shape = experts.shape
+    rows_e, experts = _read_rows(experts, len(shape) - 1, k)
     _check(lib().themis_expert_sort(rows_e, order, at, size, stream))
-    return ExpertOrder(place.view(experts.shape), counts, starts, source, capacity, order, {stream})
+    return ExpertOrder(place.view(shape), counts, starts, source, capacity, slots, shape[:-1], shape, device, order,
+                       {stream})
 
 
-def _need_rows_of(order: ExpertOrder, t: torch.Tensor, shape):
-    """t has these rows and is on the order's device."""
-    _need(t.dtype in _FLOATS and t.dim() == len(shape) + 1 and t.shape[:-1] == shape and
-          t.get_device() == order.place.get_device())
+def _slots_width(order: ExpertOrder, y: torch.Tensor) -> int:
+    shape = y.shape
+    _need(y.dtype in _FLOATS and len(shape) == 2 and shape[0] == order.slots and y.get_device() == order.device)
+    return shape[1]
+
+
+def _tokens_width(order: ExpertOrder, x: torch.Tensor) -> int:
+    shape = x.shape
+    _need(x.dtype in _FLOATS and len(shape) == len(order.pairs) and shape[:-1] == order.shape and
+          x.get_device() == order.device)
+    return shape[-1]
+
+
+def _need_weights(order: ExpertOrder, weights: torch.Tensor):
+    _need(weights.dtype in _FLOATS and weights.shape == order.pairs and weights.get_device() == order.device)
 
 
 def themis_expert_dispatch(x: torch.Tensor, order: ExpertOrder, out: Optional[torch.Tensor] = None,
@@ -846,8 +859,7 @@ def themis_expert_dispatch(x: torch.Tensor, order: ExpertOrder, out: Optional[to
     """The tokens' rows x [.., width] in the order of their experts -> [slots, width] of out's type
     (given by out or out_dtype; x's otherwise), zeros in the slots of no pair.  Its gradient is
     themis_expert_combine without weights."""
-    _need_rows_of(order, x, order.shape)
-    width = x.shape[-1]
+    width = _tokens_width(order, x)
     result = _result(out, x, (order.slots, width), out_dtype)
     if result.numel() == 0:
         return result
@@ -864,12 +876,10 @@ def themis_expert_combine(y: torch.Tensor, order: ExpertOrder, weights: Optional
     """The sum of a token's rows of y [slots, width], times weights [.., k] -> [.., width] of out's
     type (given by out or out_dtype; y's otherwise), or added to out where `accumulate`.  Pairs
     without a slot have no part."""
-    _need_rows_of(order, y, (order.slots,))
+    width = _slots_width(order, y)
     if weights is not None:
-        _need_rows_of(order, weights, order.shape)
-        _need(weights.shape == order.place.shape)
+        _need_weights(order, weights)
     _need(out is not None or not accumulate)
-    width = y.shape[-1]
     result = _result(out, y, (*order.shape, width), out_dtype)
     if result.numel() == 0:
         return result
@@ -878,7 +888,7 @@ def themis_expert_combine(y: torch.Tensor, order: ExpertOrder, weights: Optional
     rows_y, y = _read_rows(y, 1, width)
     rows_w = None
     if weights is not None:
-        rows_w, weights = _read_rows(weights, weights.dim() - 1, weights.shape[-1])
+        rows_w, weights = _read_rows(weights, len(order.shape), order.pairs[-1])
     _check(lib().themis_expert_combine(order.c_struct, rows_y, width, rows_w, int(accumulate),
                                        _written_rows(result, width), stream))
     return result
@@ -888,21 +898,19 @@ def themis_expert_combine_grad(grad_out: torch.Tensor, y: torch.Tensor, order: E
                                need_rows: bool = True, need_weights: bool = True) -> tuple:
     """The gradients behind themis_expert_combine with weights -> (of y [slots, width], of the
     weights [.., k]), each of its tensor's type, None where it is not needed."""
-    _need_rows_of(order, grad_out, order.shape)
-    _need_rows_of(order, y, (order.slots,))
-    _need_rows_of(order, weights, order.shape)
-    width = y.shape[-1]
-    _need(grad_out.shape[-1] == width and weights.shape == order.place.shape)
+    width = _slots_width(order, y)
+    _need_weights(order, weights)
+    _need(_tokens_width(order, grad_out) == width)
     stream = order.stream()
-    rows = torch.empty(y.shape, dtype=y.dtype, device=y.device) if need_rows else None
-    products = torch.empty(weights.shape, dtype=weights.dtype, device=y.device) if need_weights else None
-    rows_g, grad_out = _read_rows(grad_out, grad_out.dim() - 1, width)
+    lead, k = len(order.shape), order.pairs[-1]
+    rows = y.new_empty(y.shape) if need_rows else None
+    products = weights.new_empty(order.pairs) if need_weights else None
+    rows_g, grad_out = _read_rows(grad_out, lead, width)
     rows_y, y = _read_rows(y, 1, width)
-    rows_w, weights = _read_rows(weights, weights.dim() - 1, weights.shape[-1])
+    rows_w, weights = _read_rows(weights, lead, k)
     _check(lib().themis_expert_combine_grad(order.c_struct, rows_g, width, rows_y, rows_w,
-                                            _written_rows(rows, width) if need_rows else None,
-                                            _written_rows(products, products.shape[-1]) if need_weights else None,
-                                            stream))
+                                            _new_rows(rows, width) if need_rows else None,
+                                            _new_rows(products, k) if need_weights else None, stream))
     return rows, products
 
 
