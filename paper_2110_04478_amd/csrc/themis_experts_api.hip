@@ -159,14 +159,17 @@ int themis_expert_gate_grad(const themis_rows_t* grad_weights, const themis_rows
   if (k && (!rows_ok(grad_weights, false) || !rows_ok(experts, true))) return THEMIS_ERR_INVALID_ARGUMENT;
   if (n > kMost || n_experts > kMostExperts || k > kMostChosen) return THEMIS_ERR_UNSUPPORTED;
   if (!rows_apart(*grad_logits, n, n_experts)) return THEMIS_ERR_INVALID_ARGUMENT;
-  const GateLayout l = gate_layout((uint32_t)n_experts);
+  const GateLayout l = list_layout((uint32_t)n_experts);
   const Rows g = k ? rows_of(*grad_weights, n) : Rows{}, e = k ? rows_of(*experts, n) : Rows{};
   Launches go(stream);
   with_type(logits->type, [&](auto in) {
     with_type(grad_logits->type, [&](auto out) {
       with_own(l.own, [&](auto own) {
-        go(gate_grad_kernel<decltype(in), decltype(out), decltype(own)::value>, dim3(blocks_of(n, 256u >> l.shift)), 256, g,
-           rows_of(*logits, n), (uint32_t)n_experts, e, (uint32_t)n, (uint32_t)k, renormalize != 0,
+        constexpr int kChunks = decltype(own)::value > 4 ? 4 : decltype(own)::value;
+        typedef decltype(in) In;
+        typedef decltype(out) Out;
+        go(renormalize ? gate_grad_kernel<In, Out, kChunks, false> : gate_grad_kernel<In, Out, kChunks, true>,
+           dim3(blocks_of(n, 256u >> l.shift)), 256, g, rows_of(*logits, n), (uint32_t)n_experts, e, (uint32_t)n, (uint32_t)k,
            rows_of(*grad_logits, n), l.shift);
       });
     });
