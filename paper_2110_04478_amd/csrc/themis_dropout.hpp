@@ -51,41 +51,38 @@ __device__ __forceinline__ Floats<kVec> drop(const DropoutKey& d, const Access<k
   return x;
 }
 
-// 2^shift lanes take a row (one of its `chunks` of 256 accesses, side by side), kRows rows a lane. kOnce:
-// past the caches.
+// kRows rows a lane, one under the other: the first two rounds' products of a column, and of a row, are made
+// once.  kOnce: past the caches.
 template <bool kWhole, bool kOnce, bool kAdd, int kRows, typename In, typename Out>
 __global__ void __launch_bounds__(256)
 dropout_kernel(Rows x, uint32_t n, uint32_t width, DropoutKey d, const uint64_t* call_at, Rows add, Rows out,
-               uint32_t shift, uint32_t chunks) {
+               Spread spread) {
   constexpr int kVec = kVecOf<In, Out>;
-  const uint32_t lanes = 1u << shift, groups = 256u >> shift;
-  const uint32_t block = blockIdx.x / chunks, chunk = blockIdx.x % chunks, step = gridDim.x / chunks * groups * kRows;
-  const Access<kVec> a((chunk * 256u + (threadIdx.x & (lanes - 1u))) * kVec, width);
-  if (!a.count) return;
   if (call_at) {
     const uint64_t call = ((uint64_t)d.call[1] << 32 | d.call[0]) + *call_at;
     d.call[0] = (uint32_t)call;
     d.call[1] = (uint32_t)(call >> 32);
   }
-  for (uint64_t first = (uint64_t)block * groups * kRows + (threadIdx.x >> shift); first < n; first += step) {
+  spread_rows(spread, blockIdx.x, (n + kRows - 1) / kRows, [&](uint32_t group, uint32_t lane) {
+    const Access<kVec> a(lane * kVec, width);
     typename Packed<In, kVec>::type v[kRows];
     typename Packed<Out, kVec>::type held[kRows];
 #pragma unroll
     for (uint32_t u = 0; u < kRows; ++u) {
-      const uint32_t row = min((uint32_t)first + u * groups, n - 1u);
+      const uint32_t row = min(group * kRows + u, n - 1u);
       v[u] = a.template read<kWhole, kOnce>(row_at<const In>(x, row));
       if constexpr (kAdd) held[u] = a.template read<kWhole, kOnce>(row_at<const Out>(add, row));
     }
 #pragma unroll
     for (uint32_t u = 0; u < kRows; ++u) {
-      const uint32_t row = (uint32_t)first + u * groups;
+      const uint32_t row = group * kRows + u;
       if (row >= n) break;
       Floats<kVec> kept = drop<kVec>(d, a, row, widen<kVec>(v[u]));
       if constexpr (kAdd) kept += widen<kVec>(held[u]);
       // (its own elements and no others: x or add may be where out is)
       a.template write<kWhole, kOnce>(row_at<Out>(out, row), kept);
     }
-  }
+  });
 }
 
 }  // namespace themis

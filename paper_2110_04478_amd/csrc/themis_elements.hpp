@@ -130,6 +130,7 @@ struct Slice<8> {
   Access<8> a;
   __device__ __forceinline__ Slice(uint32_t first, uint32_t lane, uint32_t, uint32_t width) : a(first + lane * 8, width) {}
   __device__ __forceinline__ bool any() const { return a.count != 0; }
+  __device__ __forceinline__ bool whole() const { return a.count == 8; }
   template <bool kWhole, bool kOnce = false, typename T>
   __device__ __forceinline__ typename Packed<T, 8>::type read(const T* row) const { return a.read<kWhole, kOnce>(row); }
   template <bool kWhole, typename T>
@@ -145,6 +146,7 @@ struct Slice<4> {
   __device__ __forceinline__ Slice(uint32_t first, uint32_t lane, uint32_t lanes, uint32_t width)
       : a(first + lane * 4, width), b(first + (lanes + lane) * 4, width) {}
   __device__ __forceinline__ bool any() const { return a.count != 0; }
+  __device__ __forceinline__ bool whole() const { return a.count == 4 && b.count == 4; }
   template <bool kWhole, bool kOnce = false, typename T>
   __device__ __forceinline__ typename Packed<T, 8>::type read(const T* row) const {
     return __builtin_shufflevector(a.read<kWhole, kOnce>(row), b.read<kWhole, kOnce>(row), 0, 1, 2, 3, 4, 5, 6, 7);
@@ -205,6 +207,22 @@ __device__ __forceinline__ void write_zeros(uint64_t empty, uint32_t v0, uint32_
     Out* to = row_at<Out>(grad, v0 + r);
     for (uint32_t c = threadIdx.x & ((1u << shift) - 1u); c < vecs; c += 256)
       Access<kVec>(c * kVec, width).template write_over<kWhole, kAway>(to, Floats<kVec>(0.0f));
+  }
+}
+
+// Rows spread over a grid lane by lane, whatever their length: a row's `lanes` follow the one before's,
+// across wavefronts and workgroups.  Segments of rows (blockIdx.y) keep the count of lanes below 2^31.
+struct Spread {
+  uint32_t lanes, inverse, shift;   // of a row: at / lanes is (at * inverse) >> (32 + shift), of 1 at itself
+  uint32_t rows, segments;
+};
+// Calls f(row, lane) for this lane of workgroup `block`, of n rows, once for every segment.
+template <typename F>
+__device__ __forceinline__ void spread_rows(const Spread& s, uint32_t block, uint32_t n, F&& f) {
+  for (uint32_t segment = blockIdx.y; segment < s.segments; segment += gridDim.y) {
+    const uint32_t first = segment * s.rows, rows = min(n - first, s.rows), at = block * 256u + threadIdx.x;
+    const uint32_t row = s.lanes == 1 ? at : __umulhi(at, s.inverse) >> s.shift;
+    if (row < rows) f(first + row, at - row * s.lanes);
   }
 }
 

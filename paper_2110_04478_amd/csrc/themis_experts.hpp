@@ -726,107 +726,110 @@ expert_sort_kernel(Order o, Rows chosen, uint32_t part, uint32_t parts, const ui
 }
 
 // ---------------------------------------------------------------------------
-// Rows into the order of the experts and back.  2^shift lanes take a token's row (a chunk of 2,048
-// elements of a longer one: blockIdx.y), each eight elements.  A place that is no slot (-1, or what a
-// caller wrote there) is none.
+// Rows into the order of the experts and back: eight elements a lane.  A place that is no slot (-1, or
+// what a caller wrote there) is none.
 // ---------------------------------------------------------------------------
 
-// Zeros in the slots of no pair, by workgroup `block` of `blocks`.
-template <bool kWhole, typename Out>
+// sum += x * w, each element rounded once.
+__device__ __forceinline__ void add_product(float8& sum, float8 x, float w) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum[i] = __builtin_fmaf(x[i], w, sum[i]);
+}
+
+// Zeros in the slots of no pair, by workgroup `block` of `blocks`.  kAway, here and below: past the caches.
+template <bool kWhole, bool kAway, typename Out>
 __device__ __forceinline__ void clear_empty_slots(const Order& o, uint32_t block, uint32_t blocks, uint32_t rows,
                                                   uint32_t width, const Rows& out) {
   const uint32_t lane = threadIdx.x & 63u;
   for (uint64_t s0 = (uint64_t)block * rows; s0 < o.slots; s0 += (uint64_t)blocks * rows) {
     const uint32_t s = (uint32_t)s0 + lane;
     const bool empty = lane < rows && s < o.slots && (uint32_t)o.source[min(s, o.slots - 1u)] >= o.pairs;
-    write_zeros<kWhole, true, Out>(__ballot(empty), (uint32_t)s0, width, out);
+    write_zeros<kWhole, kAway, Out>(__ballot(empty), (uint32_t)s0, width, out);
   }
 }
 
 // themis_expert_dispatch: a row is read once and written to its token's slots; the first `fills`
-// workgroups clear the slots of no pair, the others take the chunks of a row side by side.
-template <bool kWhole, typename In, typename Out>
+// workgroups clear the slots of no pair.
+template <bool kWhole, bool kAway, typename In, typename Out>
 __global__ void __launch_bounds__(256)
-dispatch_kernel(Order o, Rows x, uint32_t width, Rows out, uint32_t shift, uint32_t chunks, uint32_t fills,
-                uint32_t fill_rows) {
+dispatch_kernel(Order o, Rows x, uint32_t width, Rows out, Spread spread, uint32_t fills, uint32_t fill_rows) {
   if (blockIdx.x < fills) {
-    clear_empty_slots<kWhole, Out>(o, blockIdx.x, fills, fill_rows, width, out);
+    if (blockIdx.y == 0) clear_empty_slots<kWhole, kAway, Out>(o, blockIdx.x, fills, fill_rows, width, out);
     return;
   }
-  const uint32_t lanes = 1u << shift, groups = 256u >> shift;
-  const uint32_t block = (blockIdx.x - fills) / chunks, chunk = (blockIdx.x - fills) % chunks;
-  const uint32_t blocks = (gridDim.x - fills) / chunks;
-  const Slice<kVecOf<In, Out>> slice(chunk * 256u * kLaneElements, threadIdx.x & (lanes - 1u), lanes, width);
-  if (!slice.any()) return;
-  for (uint64_t t = (uint64_t)block * groups + (threadIdx.x >> shift); t < o.n; t += (uint64_t)blocks * groups) {
-    const int32_t* place = o.place + t * o.k;
-    const float8 v = widen<8>(slice.template read<kWhole>(row_at<const In>(x, (uint32_t)t)));
+  spread_rows(spread, blockIdx.x - fills, o.n, [&](uint32_t t, uint32_t lane) {
+    const Slice<kVecOf<In, Out>> slice(0, lane, spread.lanes, width);
+    const int32_t* place = o.place + (uint64_t)t * o.k;
+    const float8 v = widen<8>(slice.template read<kWhole>(row_at<const In>(x, t)));
     for (uint32_t j = 0; j < o.k; ++j) {
       const uint32_t s = (uint32_t)place[j];
-      if (s < o.slots) slice.template write_over<kWhole, true>(row_at<Out>(out, s), v);
+      if (s < o.slots) slice.template write_over<kWhole, kAway>(row_at<Out>(out, s), v);
     }
-  }
+  });
 }
 
 // themis_expert_combine: out[t] (+)= sum over j of weights[t][j] * y[place[t][j]], kAhead rows in flight.
-constexpr uint32_t kCombineAhead = 4;
-template <bool kWhole, bool kOnce, typename In, typename Out>
+// Bound by the waits for places, then rows, which other wavefronts fill: few instructions and registers count
+// (1.07 GB of rows added to 0.13 GB 242 us; products and sums by themselves, what is added to read last 250; the next
+// token's places asked for in advance 273; eight rows in flight 301).  kOnce, here and below: y is read past the caches.
+template <bool kWhole, bool kOnce, int kAhead, typename In, typename Out>
 __global__ void __launch_bounds__(256)
-combine_kernel(Order o, Rows y, uint32_t width, Rows weights, bool accumulate, Rows out, uint32_t shift, uint32_t chunks) {
-  const uint32_t lanes = 1u << shift, groups = 256u >> shift;
-  const uint32_t block = blockIdx.x / chunks, chunk = blockIdx.x % chunks, blocks = gridDim.x / chunks;
-  const Slice<kVecOf<In, Out>> slice(chunk * 256u * kLaneElements, threadIdx.x & (lanes - 1u), lanes, width);
-  if (!slice.any()) return;
-  for (uint64_t t = (uint64_t)block * groups + (threadIdx.x >> shift); t < o.n; t += (uint64_t)blocks * groups) {
-    const int32_t* place = o.place + t * o.k;
+combine_kernel(Order o, Rows y, uint32_t width, Rows weights, bool accumulate, Rows out, Spread spread) {
+  spread_rows(spread, blockIdx.x, o.n, [&](uint32_t t, uint32_t lane) {
+    const Slice<kVecOf<In, Out>> slice(0, lane, spread.lanes, width);
+    const int32_t* place = o.place + (uint64_t)t * o.k;
+    const int64_t weights_at = row_offset(weights, t);
+    Out* to = row_at<Out>(out, t);
     float8 sum = 0.0f;
-    for (uint32_t j0 = 0; j0 < o.k; j0 += kCombineAhead) {
-      uint32_t s[kCombineAhead];
-      float w[kCombineAhead];
-      typename Packed<In, 8>::type v[kCombineAhead];
+    if (accumulate) sum = widen<8>(slice.template read<kWhole>((const Out*)to));
+    for (uint32_t j0 = 0; j0 < o.k; j0 += kAhead) {
+      uint32_t s[kAhead];
+      float w[kAhead];
+      typename Packed<In, 8>::type v[kAhead];
 #pragma unroll
-      for (uint32_t u = 0; u < kCombineAhead; ++u) {
-        const uint32_t j = min(j0 + u, o.k - 1u);
-        s[u] = j0 + u < o.k ? (uint32_t)place[j] : ~0u;
-        w[u] = weights.data ? float_at(weights, (uint32_t)t, j) : 1.0f;
+      for (uint32_t u = 0; u < kAhead; ++u) s[u] = j0 + u < o.k ? (uint32_t)place[j0 + u] : ~0u;
+#pragma unroll
+      for (uint32_t u = 0; u < kAhead; ++u) {
+        w[u] = 1.0f;
+        if (weights.data && j0 + u < o.k)
+          w[u] = weights.type == THEMIS_F32 ? ((const float*)weights.data)[weights_at + j0 + u] : float_at(weights, t, j0 + u);
       }
 #pragma unroll
-      for (uint32_t u = 0; u < kCombineAhead; ++u) {
+      for (uint32_t u = 0; u < kAhead; ++u) {
         v[u] = {};
         if (s[u] < o.slots) v[u] = slice.template read<kWhole, kOnce>(row_at<const In>(y, s[u]));
       }
 #pragma unroll
-      for (uint32_t u = 0; u < kCombineAhead; ++u)
-        if (s[u] < o.slots) sum += widen<8>(v[u]) * w[u];
+      for (uint32_t u = 0; u < kAhead; ++u) add_product(sum, widen<8>(v[u]), s[u] < o.slots ? w[u] : 0.0f);
     }
-    Out* to = row_at<Out>(out, (uint32_t)t);
-    if (accumulate) sum += widen<8>(slice.template read<kWhole>((const Out*)to));
     slice.template write<kWhole>(to, sum);
-  }
+  });
 }
 
 // themis_expert_combine_grad: rows[s] = weights[a] * grad[t] and weights'[a] = <grad[t], y[s]> for the pair
-// a = (t, j) in slot s.  2^shift lanes (up to a wavefront) take kPairs of a token's pairs over the whole
-// row, so that a product is summed where it is made.
-template <bool kWhole, bool kOnce, typename G, typename Y, int kPairs>
+// a = (t, j) in slot s.  2^shift lanes (up to a wavefront) take two of a token's pairs over the whole row, so
+// that a product is summed where it is made.  Bound by memory and by its instructions: 268 MB of rows of 4,096 bf16
+// read and 335 written 132 us (5.6 TB/s); one pair or four for a wavefront cost up to 29 % and 7 % more.
+constexpr uint32_t kGradPairs = 2;
+template <bool kWhole, bool kOnce, bool kAway, typename G, typename Y>
 __global__ void __launch_bounds__(256)
 combine_grad_kernel(Order o, Rows grad, uint32_t width, Rows y, Rows weights, Rows rows, Rows grad_weights, uint32_t shift,
                     uint32_t fills, uint32_t fill_rows) {
   if (blockIdx.x < fills) {
-    clear_empty_slots<kWhole, Y>(o, blockIdx.x, fills, fill_rows, width, rows);
+    clear_empty_slots<kWhole, kAway, Y>(o, blockIdx.x, fills, fill_rows, width, rows);
     return;
   }
-  const uint32_t lanes = 1u << shift, lane = threadIdx.x & (lanes - 1u), each = (o.k + kPairs - 1) / kPairs;
+  const uint32_t lanes = 1u << shift, lane = threadIdx.x & (lanes - 1u), each = (o.k + kGradPairs - 1) / kGradPairs;
   const uint32_t groups = 256u >> shift, block = blockIdx.x - fills, blocks = gridDim.x - fills;
   const uint64_t units = (uint64_t)o.n * each;
   for (uint64_t u0 = (uint64_t)block * groups; u0 < units; u0 += (uint64_t)blocks * groups) {
     const uint64_t unit = u0 + (threadIdx.x >> shift);
     const bool mine = unit < units;
-    const uint32_t t = mine ? (uint32_t)(unit / each) : 0u, j0 = mine ? (uint32_t)(unit % each) * kPairs : 0u;
-    uint32_t s[kPairs];
-    float w[kPairs], dot[kPairs];
+    const uint32_t t = mine ? (uint32_t)(unit / each) : 0u, j0 = mine ? (uint32_t)(unit % each) * kGradPairs : 0u;
+    uint32_t s[kGradPairs];
+    float w[kGradPairs], dot[kGradPairs];
 #pragma unroll
-    for (uint32_t u = 0; u < kPairs; ++u) {
+    for (uint32_t u = 0; u < kGradPairs; ++u) {
       const uint32_t j = min(j0 + u, o.k - 1u);
       s[u] = mine && j0 + u < o.k ? (uint32_t)o.place[(uint64_t)t * o.k + j] : ~0u;
       w[u] = float_at(weights, t, j);
@@ -836,23 +839,30 @@ combine_grad_kernel(Order o, Rows grad, uint32_t width, Rows y, Rows weights, Ro
       const Slice<kVecOf<G, Y>> slice(c, lane, lanes, width);
       if (!slice.any()) continue;
       const float8 g = widen<8>(slice.template read<kWhole>(row_at<const G>(grad, t)));
-      typename Packed<Y, 8>::type v[kPairs];
+      // (other lanes' elements: a choice for the wavefront, since most have none and instructions count)
+      const bool whole = !__ballot(!slice.whole());
+      typename Packed<Y, 8>::type v[kGradPairs];
 #pragma unroll
-      for (uint32_t u = 0; u < kPairs; ++u) {
+      for (uint32_t u = 0; u < kGradPairs; ++u) {
         v[u] = {};
         if (grad_weights.data && s[u] < o.slots) v[u] = slice.template read<kWhole, kOnce>(row_at<const Y>(y, s[u]));
       }
 #pragma unroll
-      for (uint32_t u = 0; u < kPairs; ++u) {
+      for (uint32_t u = 0; u < kGradPairs; ++u) {
         if (s[u] >= o.slots) continue;
-        if (rows.data) slice.template write_over<kWhole, true>(row_at<Y>(rows, s[u]), g * w[u]);
-        const float8 p = slice.template own<kWhole>(g * widen<8>(v[u]));
-        dot[u] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        if (rows.data) slice.template write_over<kWhole, kAway>(row_at<Y>(rows, s[u]), g * w[u]);
+        float8 x = widen<8>(v[u]), mine = g;
+        if (!whole) {
+          x = slice.template own<kWhole>(x);
+          mine = slice.template own<kWhole>(mine);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dot[u] = __builtin_fmaf(x[i], mine[i], dot[u]);
       }
     }
     if (!grad_weights.data) continue;
 #pragma unroll
-    for (uint32_t u = 0; u < kPairs; ++u) {
+    for (uint32_t u = 0; u < kGradPairs; ++u) {
       const float sum = group_sum(dot[u], shift);
       if (mine && lane == 0 && j0 + u < o.k) put_float(grad_weights, t, j0 + u, sum);
     }

@@ -14,7 +14,7 @@ namespace themis {
 namespace {
 
 constexpr uint64_t kLastCache = 256u << 20;   // bytes of the last cache level
-constexpr uint64_t kMostWidth = 1u << 25;   // (2^15 chunks of a row at most, side by side in a grid)
+constexpr uint64_t kMostWidth = 1u << 25;
 
 // Lanes of a token's logits, 2^shift of `own` each.
 struct GateLayout { uint32_t own, shift; };
@@ -76,17 +76,18 @@ bool target_ok(const themis_rows_t* r, uint64_t n, uint64_t width, bool index = 
   return rows_ok(r, index) && rows_apart(*r, n, width);
 }
 
-// How a row of `width` elements is spread over lanes and columns of workgroups.
-struct RowLayout { uint32_t shift, chunks; };
-RowLayout row_layout(uint64_t width, uint32_t vec = kLaneElements) {
-  const uint32_t vecs = (uint32_t)((width + vec - 1) / vec);
-  return {std::min(next_power(vecs), 8u), (vecs + 255) / 256};
+// n rows of `width` elements over a grid, `vec` elements a lane.  (Lanes in powers of two for a row: 65 of 128 have
+// work in rows of 520, whose sums of eight take 121 us in place of 99.)
+Spread spread_of(uint64_t n, uint64_t width, uint32_t vec) {
+  // (of numbers below 2^31 the quotient is exact: inverse exceeds 2^(31 + power) / lanes by less than one, and
+  // lanes are at most 2^power)
+  const uint32_t lanes = (uint32_t)((width + vec - 1) / vec), power = next_power(lanes);
+  const uint32_t rows = (uint32_t)std::min<uint64_t>(n, (kMost - 256) / lanes);
+  return {lanes, (uint32_t)(((1ull << (31 + power)) + lanes - 1) / lanes), power ? power - 1 : 0, rows,
+          (uint32_t)((n + rows - 1) / rows)};
 }
-
-// Workgroups where a row's chunks are side by side.  (8 KiB rows into the order: 217 us, one chunk of all rows
-// after the other 221.)
-uint32_t chunk_blocks(uint64_t n, RowLayout l) {
-  return l.chunks * (uint32_t)std::min<uint64_t>((n + (256u >> l.shift) - 1) / (256u >> l.shift), std::max(1u, (1u << 22) / l.chunks));
+dim3 grid_of(const Spread& s, uint32_t more = 0) {
+  return dim3(more + (uint32_t)(((uint64_t)s.rows * s.lanes + 255) / 256), std::min(s.segments, 65535u));
 }
 
 // Rows of experts that the last cache level cannot hold are read past it (1.07 GB: sums 229 us, through it
@@ -94,6 +95,9 @@ uint32_t chunk_blocks(uint64_t n, RowLayout l) {
 bool read_once(const Order& o, uint64_t width, int type) {
   return (uint64_t)std::min(o.slots, o.pairs) * width * type_bytes(type) >= kLastCache;
 }
+
+// Whether rows of `width` elements are whole lines of the caches.
+bool whole_lines(const Rows& r, uint64_t width) { return width * type_bytes(r.type) % 128 == 0 && aligned(r.data, 128); }
 
 // Slots of a workgroup that looks for those of no pair: about 256 KiB.
 uint32_t slots_to_clear(uint64_t row_bytes) {
@@ -207,7 +211,7 @@ int themis_expert_dispatch(const themis_expert_order_t* order, const themis_rows
   if ((o.n && !rows_ok(x, false)) || !rows_ok(out, false)) return THEMIS_ERR_INVALID_ARGUMENT;
   if (width > kMostWidth) return THEMIS_ERR_UNSUPPORTED;
   if (!rows_apart(*out, o.slots, width)) return THEMIS_ERR_INVALID_ARGUMENT;
-  const RowLayout l = row_layout(width);
+  const Spread spread = o.n ? spread_of(o.n, width, kLaneElements) : Spread{};
   const Rows from = o.n ? rows_of(*x, o.n) : Rows{0, 0, 0, 0, out->type}, to = rows_of(*out, o.slots);
   const uint32_t fill_rows = slots_to_clear(width * type_bytes(to.type)), fills = blocks_of(o.slots, fill_rows);
   Launches go(stream);
@@ -215,8 +219,12 @@ int themis_expert_dispatch(const themis_expert_order_t* order, const themis_rows
     with_type(to.type, [&](auto out) {
       typedef decltype(in) In;
       typedef decltype(out) Out;
-      go(width < kLaneElements ? dispatch_kernel<false, In, Out> : dispatch_kernel<true, In, Out>,
-         dim3(fills + chunk_blocks(o.n, l)), 256, o, from, (uint32_t)width, to, l.shift, l.chunks, fills, fill_rows);
+      // Whole lines go past the caches (65,536 rows of 2,048 to 50 MB .. 320 MB: 13 % less), others, which two rows
+      // share, do not (100,000 rows of 1,001 bf16: 47 us, past them 57).
+      go(width < kLaneElements     ? dispatch_kernel<false, false, In, Out>
+         : whole_lines(to, width) ? dispatch_kernel<true, true, In, Out>
+                                   : dispatch_kernel<true, false, In, Out>,
+         o.n ? grid_of(spread, fills) : dim3(fills), 256, o, from, (uint32_t)width, to, spread, fills, fill_rows);
     });
   });
   return go.status();
@@ -231,7 +239,7 @@ int themis_expert_combine(const themis_expert_order_t* order, const themis_rows_
   if (weights && o.k && !rows_ok(weights, false)) return THEMIS_ERR_INVALID_ARGUMENT;
   if (width > kMostWidth) return THEMIS_ERR_UNSUPPORTED;
   if (!rows_apart(*out, o.n, width)) return THEMIS_ERR_INVALID_ARGUMENT;
-  const RowLayout l = row_layout(width);
+  const Spread spread = spread_of(o.n, width, kLaneElements);
   const Rows from = o.slots ? rows_of(*y, o.slots) : Rows{0, 0, 0, 0, out->type}, to = rows_of(*out, o.n);
   const bool once = read_once(o, width, from.type);
   Launches go(stream);
@@ -239,11 +247,18 @@ int themis_expert_combine(const themis_expert_order_t* order, const themis_rows_
     with_type(to.type, [&](auto out) {
       typedef decltype(in) In;
       typedef decltype(out) Out;
-      go(width < kLaneElements ? combine_kernel<false, false, In, Out>
-         : once                ? combine_kernel<true, true, In, Out>
-                               : combine_kernel<true, false, In, Out>,
-         dim3(chunk_blocks(o.n, l)), 256, o, from, (uint32_t)width, rows_or_none(weights, o.n), accumulate != 0, to, l.shift,
-         l.chunks);
+      auto run = [&](auto kernel) {
+        go(kernel, grid_of(spread), 256, o, from, (uint32_t)width, rows_or_none(weights, o.n), accumulate != 0, to, spread);
+      };
+      auto turns_of = [&](auto ahead) {
+        constexpr int kAhead = decltype(ahead)::value;
+        if (width < kLaneElements) run(combine_kernel<false, false, kAhead, In, Out>);
+        else if (once) run(combine_kernel<true, true, kAhead, In, Out>);
+        else run(combine_kernel<true, false, kAhead, In, Out>);
+      };
+      // (16,384 tokens of 5,120, k = 2: 104 us, with four rows in flight 122)
+      if (o.k <= 2) turns_of(std::integral_constant<int, 2>{});
+      else turns_of(std::integral_constant<int, 4>{});
     });
   });
   return go.status();
@@ -269,23 +284,22 @@ int themis_expert_combine_grad(const themis_expert_order_t* order, const themis_
   const Rows g = o.pairs && width ? rows_of(*grad_out, o.n) : Rows{0, 0, 0, 0, from.type};
   const uint32_t fill_rows = rows ? slots_to_clear(width * type_bytes(to.type)) : 1u;
   const uint32_t fills = rows ? blocks_of(o.slots, fill_rows) : 0u;
-  const uint32_t shift = std::min(row_layout(std::max<uint64_t>(width, 1)).shift, 6u);
+  const uint32_t shift = std::min(next_power((uint32_t)((width + kLaneElements - 1) / kLaneElements)), 6u);
   const bool once = read_once(o, width, from.type);
+  // (rows past the caches: 537 MB 213 us, through them 220; 335 MB 136 and 120)
+  const bool away = rows && whole_lines(to, width) && (uint64_t)o.slots * width * type_bytes(to.type) >= 2 * kLastCache;
   Launches go(stream);
   with_type(g.type, [&](auto grad) {
     with_type(from.type, [&](auto row) {
       typedef decltype(grad) G;
       typedef decltype(row) Y;
-      auto run = [&](auto kernel, uint32_t pairs) {
-        go(kernel, dim3(fills + blocks_of((uint64_t)o.n * ((o.k + pairs - 1) / pairs), 256u >> shift)), 256, o, g,
-           (uint32_t)width, from, o.pairs ? rows_of(*weights, o.n) : Rows{}, to,
-           products ? rows_of(*grad_weights, o.n) : Rows{}, shift, fills, fill_rows);
-      };
-      // Four pairs of a token where a wavefront has their rows in one turn (65,536 tokens of 512, k = 8: 229 us,
-      // with two 257), two of longer rows, for more wavefronts (16,384 of 2,048: 214, with four 224).
-      if (width < kLaneElements) run(combine_grad_kernel<false, false, G, Y, 2>, 2);
-      else if (width <= 512 && o.k > 2) run(once ? combine_grad_kernel<true, true, G, Y, 4> : combine_grad_kernel<true, false, G, Y, 4>, 4);
-      else run(once ? combine_grad_kernel<true, true, G, Y, 2> : combine_grad_kernel<true, false, G, Y, 2>, 2);
+      go(width < kLaneElements ? combine_grad_kernel<false, false, false, G, Y>
+         : once && away        ? combine_grad_kernel<true, true, true, G, Y>
+         : once                ? combine_grad_kernel<true, true, false, G, Y>
+                               : combine_grad_kernel<true, false, false, G, Y>,
+         dim3(fills + blocks_of((uint64_t)o.n * ((o.k + kGradPairs - 1) / kGradPairs), 256u >> shift)), 256, o, g,
+         (uint32_t)width, from, o.pairs ? rows_of(*weights, o.n) : Rows{}, to,
+         products ? rows_of(*grad_weights, o.n) : Rows{}, shift, fills, fill_rows);
     });
   });
   return go.status();
@@ -307,15 +321,15 @@ int themis_dropout(const themis_rows_t* x, uint64_t n, uint64_t width, double p,
     with_type(out->type, [&](auto to) {
       typedef decltype(in) In;
       typedef decltype(to) Out;
-      const RowLayout l = row_layout(width, kVecOf<In, Out>);
       // What the last cache level cannot hold goes past it, and two rows of 16 bits a lane are in flight then
       // (268 M bf16: 169 us, otherwise 194; with a residual 256, 285; 50 M 19 and 18; binary32 with a residual, 134 M,
       // one row 269, two 286, through the caches 292).
       const bool once = n * width * (type_bytes(x->type) + type_bytes(out->type)) >= kLastCache;
       constexpr int kTwo = sizeof(In) == 2 && sizeof(Out) == 2 ? 2 : 1;
       auto run = [&](auto kernel, uint32_t rows) {
-        go(kernel, dim3(chunk_blocks((n + rows - 1) / rows, l)), 256, rows_of(*x, n), (uint32_t)n, (uint32_t)width, d, call_at,
-           rows_or_none(add, n), rows_of(*out, n), l.shift, l.chunks);
+        const Spread spread = spread_of((n + rows - 1) / rows, width, kVecOf<In, Out>);
+        go(kernel, grid_of(spread), 256, rows_of(*x, n), (uint32_t)n, (uint32_t)width, d, call_at, rows_or_none(add, n),
+           rows_of(*out, n), spread);
       };
       auto adds = [&](auto is) {
         constexpr bool kAdd = decltype(is)::value;
