@@ -6,7 +6,10 @@ buckets that the ranks' All-Reduces carry, and clips what comes back by the norm
 parameters are updated from the buckets.  The sizes of the buckets are then a trace for the evaluator: it
 plans and simulates the iteration's All-Reduces on the six platforms of the paper's Table 2.
 
-    python examples/training_iteration.py [steps]
+With experts the feed-forward layer is one of experts in buffers of a fixed capacity, whose gradients go into the
+same buckets; with dropout what the layer adds to the residual is dropped by a counter.
+
+    python examples/training_iteration.py [steps [experts [dropout]]]
 """
 import math
 import os
@@ -17,26 +20,44 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
-from paper_2110_04478_amd import binding, workloads  # noqa: E402
+from paper_2110_04478_amd import binding, layers, workloads  # noqa: E402
 from paper_2110_04478_amd.gradients import GradientBuckets, embedding  # noqa: E402
 
 PAD = 0
+CHOSEN, CAPACITY = 2, 1.5   # experts of a token; an expert's buffer over the mean load
+SEED = 11
 
 
-def model(vocab, width, device, seed):
+def model(vocab, width, device, seed, experts=0):
     g = torch.Generator().manual_seed(seed)
 
     def weight(*shape):
         return torch.nn.Parameter((torch.randn(shape, generator=g) / math.sqrt(shape[-1])).to(device))
 
+    if experts:
+        return dict(table=weight(vocab, width), router=weight(experts, width), up=weight(experts, width, 4 * width),
+                    down=weight(experts, 4 * width, width))
     return dict(table=weight(vocab, width), up=weight(4 * width, width), down=weight(width, 4 * width))
 
 
-def loss_of(p, tokens):
+def feed_forward(p, x):
+    if "router" not in p:
+        return torch.relu(x @ p["up"].t()) @ p["down"].t()
+    n_experts, width = p["up"].shape[:2]
+    capacity = math.ceil(CAPACITY * CHOSEN * x[..., 0].numel() / n_experts)
+    weights, chosen = layers.gate(x @ p["router"].t(), CHOSEN)
+    order = layers.sort(chosen, n_experts, capacity)
+    rows = layers.dispatch(x, order).view(n_experts, capacity, width)
+    rows = torch.bmm(torch.relu(torch.bmm(rows, p["up"])), p["down"])
+    return layers.combine(rows.view(order.slots, width), order, weights)
+
+
+def loss_of(p, tokens, dropout=0.0, step=0):
     """Next-token loss; padding is looked up but has no gradient and is not predicted."""
     width = p["table"].shape[1]
     x = embedding(p["table"], tokens[:, :-1], math.sqrt(width), ignored=PAD, into=p["table"].grad)
-    x = x + torch.relu(x @ p["up"].t()) @ p["down"].t()
+    y = feed_forward(p, x)
+    x = layers.dropout(y, dropout, SEED, step, add=x) if dropout else x + y
     x = x / (x.square().mean(-1, keepdim=True) + 1e-6).sqrt()
     logits = x @ p["table"].t()
     return torch.nn.functional.cross_entropy(logits.flatten(0, 1), tokens[:, 1:].flatten(), ignore_index=PAD)
@@ -70,14 +91,14 @@ def iteration_times(sizes, chunks=64):
 
 
 def main(steps=40, vocab=2000, width=256, batch=16, length=128, rate=2.0, max_norm=1.0, device="cuda:0",
-         all_reduce=lambda buckets: None):
+         all_reduce=lambda buckets: None, experts=0, dropout=0.0):
     """all_reduce: sums the buckets over the ranks, in place (one rank: they are the sum)."""
-    p = model(vocab, width, device, 1)
+    p = model(vocab, width, device, 1, experts)
     buckets = GradientBuckets(p.values(), bucket_bytes=1 << 20)
     losses, norms = [], []
     for step in range(steps):
         buckets.zero()
-        loss = loss_of(p, batch_of(vocab, batch, length, device, step))
+        loss = loss_of(p, batch_of(vocab, batch, length, device, step), dropout, step)
         loss.backward()
         buckets.fill()
         all_reduce(buckets.buckets)
@@ -92,7 +113,8 @@ def main(steps=40, vocab=2000, width=256, batch=16, length=128, rate=2.0, max_no
 
 
 if __name__ == "__main__":
-    got = main(int(sys.argv[1]) if len(sys.argv) > 1 else 40)
+    got = main(int(sys.argv[1]) if len(sys.argv) > 1 else 40, experts=int(sys.argv[2]) if len(sys.argv) > 2 else 0,
+               dropout=float(sys.argv[3]) if len(sys.argv) > 3 else 0.0)
     print("loss %.3f -> %.3f, norm of the gradients %.3f -> %.3f" %
           (got["losses"][0], got["losses"][-1], got["norms"][0], got["norms"][-1]))
     print("buckets of the iteration, bytes: %s" % ", ".join("%d" % s for s in got["sizes"]))
