@@ -193,7 +193,7 @@ gate_kernel(Rows logits, uint32_t experts, uint32_t n, uint32_t k, bool renormal
 // An entry is a number that is ordered as (logit, index from the end) is: of logits of 16 bits
 // a whole number, the logit as a signed one (so that -0 is 0) over its index, of binary32 a binary64
 // number, the logit with its index in the last of the 29 bits that it leaves free.
-// 65,536 tokens on 256 experts, eight of them (bf16): 13.4 us, of which the logits' bytes need 8; by k
+// 65,536 tokens on 256 experts, eight of them (bf16): 12.8 us, of which the logits' bytes need 8; by k
 // rounds of a maximum 33.
 // ---------------------------------------------------------------------------
 constexpr uint32_t kMostListed = 8;
@@ -775,7 +775,7 @@ dispatch_kernel(Order o, Rows x, uint32_t width, Rows out, Spread spread, uint32
 
 // themis_expert_combine: out[t] (+)= sum over j of weights[t][j] * y[place[t][j]], kAhead rows in flight.
 // Bound by the waits for places, then rows, which other wavefronts fill: few instructions and registers count
-// (1.07 GB of rows added to 0.13 GB 242 us; products and sums by themselves, what is added to read last 250; the next
+// (1.07 GB of rows added to 0.13 GB 238 us; products and sums by themselves, what is added to read last 250; the next
 // token's places asked for in advance 273; eight rows in flight 301).  kOnce, here and below: y is read past the caches.
 template <bool kWhole, bool kOnce, int kAhead, typename In, typename Out>
 __global__ void __launch_bounds__(256)
@@ -814,7 +814,7 @@ combine_kernel(Order o, Rows y, uint32_t width, Rows weights, bool accumulate, R
 // themis_expert_combine_grad: rows[s] = weights[a] * grad[t] and weights'[a] = <grad[t], y[s]> for the pair
 // a = (t, j) in slot s.  2^shift lanes (up to a wavefront) take two of a token's pairs over the whole row, so
 // that a product is summed where it is made.  Bound by memory and by its instructions: 268 MB of rows of 4,096 bf16
-// read and 335 written 132 us (5.6 TB/s); one pair or four for a wavefront cost up to 29 % and 7 % more.
+// read and 335 written 135 us (5.5 TB/s); one pair or four for a wavefront cost up to 29 % and 7 % more.
 constexpr uint32_t kGradPairs = 2;
 template <bool kWhole, bool kOnce, bool kAway, typename G, typename Y>
 __global__ void __launch_bounds__(256)

@@ -77,7 +77,7 @@ bool target_ok(const themis_rows_t* r, uint64_t n, uint64_t width, bool index = 
 }
 
 // n rows of `width` elements over a grid, `vec` elements a lane.  (Lanes in powers of two for a row: 65 of 128 have
-// work in rows of 520, whose sums of eight take 121 us in place of 99.)
+// work in rows of 520, whose sums of eight take 121 us in place of 97.)
 Spread spread_of(uint64_t n, uint64_t width, uint32_t vec) {
   // (of numbers below 2^31 the quotient is exact: inverse exceeds 2^(31 + power) / lanes by less than one, and
   // lanes are at most 2^power)
@@ -90,8 +90,8 @@ dim3 grid_of(const Spread& s, uint32_t more = 0) {
   return dim3(more + (uint32_t)(((uint64_t)s.rows * s.lanes + 255) / 256), std::min(s.segments, 65535u));
 }
 
-// Rows of experts that the last cache level cannot hold are read past it (1.07 GB: sums 229 us, through it
-// 255; 335 MB: gradients 115, 138); the others may still be there (200 MB: 28 us, 24).
+// Rows of experts that the last cache level cannot hold are read past it (1.07 GB: sums 242 us, through it
+// 253; 537 MB of binary32 122, 145); the others may still be there (200 MB: 28 us, 24).
 bool read_once(const Order& o, uint64_t width, int type) {
   return (uint64_t)std::min(o.slots, o.pairs) * width * type_bytes(type) >= kLastCache;
 }
@@ -219,8 +219,8 @@ int themis_expert_dispatch(const themis_expert_order_t* order, const themis_rows
     with_type(to.type, [&](auto out) {
       typedef decltype(in) In;
       typedef decltype(out) Out;
-      // Whole lines go past the caches (65,536 rows of 2,048 to 50 MB .. 320 MB: 13 % less), others, which two rows
-      // share, do not (100,000 rows of 1,001 bf16: 47 us, past them 57).
+      // Whole lines go past the caches (65,536 rows of 2,048 bf16: 50 us, through them 58), others, which two rows
+      // share, do not (100,000 rows of 1,001: 47 us, past them 57).
       go(width < kLaneElements     ? dispatch_kernel<false, false, In, Out>
          : whole_lines(to, width) ? dispatch_kernel<true, true, In, Out>
                                    : dispatch_kernel<true, false, In, Out>,
@@ -256,7 +256,7 @@ int themis_expert_combine(const themis_expert_order_t* order, const themis_rows_
         else if (once) run(combine_kernel<true, true, kAhead, In, Out>);
         else run(combine_kernel<true, false, kAhead, In, Out>);
       };
-      // (16,384 tokens of 5,120, k = 2: 104 us, with four rows in flight 122)
+      // (20,480 tokens of 5,120 bf16, k = 2: 108 us, with four rows in flight 122)
       if (o.k <= 2) turns_of(std::integral_constant<int, 2>{});
       else turns_of(std::integral_constant<int, 4>{});
     });
@@ -286,8 +286,9 @@ int themis_expert_combine_grad(const themis_expert_order_t* order, const themis_
   const uint32_t fills = rows ? blocks_of(o.slots, fill_rows) : 0u;
   const uint32_t shift = std::min(next_power((uint32_t)((width + kLaneElements - 1) / kLaneElements)), 6u);
   const bool once = read_once(o, width, from.type);
-  // (rows past the caches: 537 MB 213 us, through them 220; 335 MB 136 and 120)
-  const bool away = rows && whole_lines(to, width) && (uint64_t)o.slots * width * type_bytes(to.type) >= 2 * kLastCache;
+  // (rows past the caches: 268 MB 110 us, through them 125; 410 MB 178 and 187; rows that share
+  // lines take 7 to 10 % more that way)
+  const bool away = rows && whole_lines(to, width) && (uint64_t)o.slots * width * type_bytes(to.type) >= kLastCache;
   Launches go(stream);
   with_type(g.type, [&](auto grad) {
     with_type(from.type, [&](auto row) {
