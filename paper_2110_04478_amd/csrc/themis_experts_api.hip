@@ -16,27 +16,22 @@ namespace {
 constexpr uint64_t kLastCache = 256u << 20;   // bytes of the last cache level
 constexpr uint64_t kMostWidth = 1u << 25;
 
-// Lanes of a token's logits, 2^shift of `own` each.
+// Lanes of a token's logits: 2^shift of `own` each; where lists are kept, of `own` times eight.  (More than
+// kMostListed chosen: nine experts at least.)
 struct GateLayout { uint32_t own, shift; };
 GateLayout gate_layout(uint32_t experts) {
-  GateLayout l = {8, kGateLeastShift};
-  if (experts > 512) l = {16, 6};
-  else if (experts > 64) l.shift = next_power((experts + 7) / 8);
-  else l.own = experts <= 8 ? 1 : experts <= 16 ? 2 : experts <= 32 ? 4 : 8;
-  return l;
+  if (experts > 512) return {16, 6};
+  if (experts > 64) return {8, next_power((experts + 7) / 8)};
+  return {experts <= 16 ? 2u : experts <= 32 ? 4u : 8u, kGateLeastShift};
 }
-// The same where lists are kept: 2^shift lanes of `chunks` times eight.
 GateLayout list_layout(uint32_t experts) {
   const uint32_t chunks = experts <= 64 ? 1 : experts <= 128 ? 2 : 4;
   return {chunks, next_power((experts + 8 * chunks - 1) / (8 * chunks))};
 }
-template <typename F>
+// Calls f with `own` as a constant, one of kOwn.
+template <int... kOwn, typename F>
 void with_own(uint32_t own, F&& f) {
-  if (own == 1) f(std::integral_constant<int, 1>{});
-  else if (own == 2) f(std::integral_constant<int, 2>{});
-  else if (own == 4) f(std::integral_constant<int, 4>{});
-  else if (own == 8) f(std::integral_constant<int, 8>{});
-  else f(std::integral_constant<int, 16>{});
+  ((own == kOwn ? f(std::integral_constant<int, kOwn>{}) : void()), ...);
 }
 
 uint32_t blocks_of(uint64_t n, uint64_t each) { return (uint32_t)std::min<uint64_t>((n + each - 1) / each, 1u << 20); }
@@ -130,8 +125,8 @@ int themis_expert_gate(const themis_rows_t* logits, uint64_t n_experts, uint64_t
     };
     with_type(logits->type, [&](auto in) {
       typedef decltype(in) In;
-      with_own(m.own, [&](auto own) {
-        constexpr int kChunks = decltype(own)::value > 4 ? 4 : decltype(own)::value;
+      with_own<1, 2, 4>(m.own, [&](auto own) {
+        constexpr int kChunks = decltype(own)::value;
         auto over = [&](auto all) {
           constexpr bool kAll = decltype(all)::value;
           if (k == 1) run(gate_list_kernel<In, kChunks, 1, kAll>);
@@ -146,7 +141,7 @@ int themis_expert_gate(const themis_rows_t* logits, uint64_t n_experts, uint64_t
     return go.status();
   }
   with_type(logits->type, [&](auto in) {
-    with_own(l.own, [&](auto own) {
+    with_own<2, 4, 8, 16>(l.own, [&](auto own) {
       go(gate_kernel<decltype(in), decltype(own)::value>, dim3(blocks_of(n, 256u >> l.shift)), 256, rows_of(*logits, n),
          (uint32_t)n_experts, (uint32_t)n, (uint32_t)k, renormalize != 0, rows_of(*weights, n), rows_of(*experts, n),
          l.shift);
@@ -168,8 +163,8 @@ int themis_expert_gate_grad(const themis_rows_t* grad_weights, const themis_rows
   Launches go(stream);
   with_type(logits->type, [&](auto in) {
     with_type(grad_logits->type, [&](auto out) {
-      with_own(l.own, [&](auto own) {
-        constexpr int kChunks = decltype(own)::value > 4 ? 4 : decltype(own)::value;
+      with_own<1, 2, 4>(l.own, [&](auto own) {
+        constexpr int kChunks = decltype(own)::value;
         typedef decltype(in) In;
         typedef decltype(out) Out;
         go(renormalize ? gate_grad_kernel<In, Out, kChunks, false> : gate_grad_kernel<In, Out, kChunks, true>,

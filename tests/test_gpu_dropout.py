@@ -47,10 +47,11 @@ def test_the_generators_published_answers():
         assert " ".join("%08x" % int(x) for x in philox(counter, key)) == want
 
 
-def kept_of(rows, width, p, seed, call):
+def kept_of(rows, width, p, seed, call, first=0):
+    """Of the rows from `first` on."""
     seed, call, low = seed % 2 ** 64, call % 2 ** 64, 0xFFFFFFFF
     blocks = -(-width // 4)
-    c0, c1 = np.meshgrid(np.arange(blocks, dtype=np.uint64), np.arange(rows, dtype=np.uint64))
+    c0, c1 = np.meshgrid(np.arange(blocks, dtype=np.uint64), np.arange(first, first + rows, dtype=np.uint64))
     words = philox((c0, c1, np.full_like(c0, call & low), np.full_like(c0, call >> 32)), (seed & low, seed >> 32))
     return np.stack(words, -1).reshape(rows, -1)[:, :width] >= round(p * 2.0 ** 32)
 
@@ -165,6 +166,18 @@ def test_more_than_the_last_cache_level_holds(gpu, kind, width, n):
         out = x.clone() if add is None else add.clone()
         gpu.themis_dropout(out if add is None else x, 0.3, 3, 4, add=None if add is None else out, out=out)
         same(out, got)
+
+
+def test_more_rows_than_a_grid_has_lanes(gpu):
+    """1.07 G rows of nine elements, two lanes each: in two segments."""
+    n, width = (2 ** 31 - 257) // 2 + 3000, 9
+    x = torch.arange(1.0, 10.0).cuda().expand(n, width)
+    got = gpu.themis_dropout(x, 0.4, 8, 9, out_dtype=BF16)
+    scale = float(np.float32(1 / (1 - 0.4)))
+    for first in (0, 10 ** 9, n - 3500, n - 100):
+        kept = torch.from_numpy(kept_of(100, width, 0.4, 8, 9, first))
+        want = torch.where(kept, torch.arange(1.0, 10.0) * scale, 0.0).to(BF16)
+        same(got[first:first + 100], want)
 
 
 def test_nothing(gpu):

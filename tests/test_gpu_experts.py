@@ -463,6 +463,41 @@ def test_infinite_neighbours_stay_out_of_products(gpu):
         assert torch.equal(torch.isnan(products.cpu()), torch.isnan(want))
 
 
+def test_rows_without_pairs(gpu):
+    """No experts a token, no tokens, no slots that anybody has, no columns."""
+    order = gpu.themis_expert_sort(torch.zeros((6, 0), dtype=I32).cuda(), 3, 2)
+    x = normal((6, 20), BF16, 1).cuda()
+    assert not gpu.themis_expert_dispatch(x, order).any()
+    assert not gpu.themis_expert_combine(normal((6, 20), BF16, 2).cuda(), order).any()
+    held = x.clone()
+    assert torch.equal(gpu.themis_expert_combine(normal((6, 20), BF16, 2).cuda(), order, out=held, accumulate=True), x)
+    rows, products = gpu.themis_expert_combine_grad(x, normal((6, 20), BF16, 3).cuda(), order, torch.zeros(6, 0).cuda())
+    assert not rows.any() and products.shape == (6, 0)
+    order = gpu.themis_expert_sort(torch.zeros((0, 2), dtype=I32).cuda(), 3, 2)
+    assert not gpu.themis_expert_dispatch(x[:0], order).any()
+    assert gpu.themis_expert_combine(x, order).shape == (0, 20)
+    order = gpu.themis_expert_sort(torch.full((6, 2), -1, dtype=I32).cuda(), 3)
+    assert not gpu.themis_expert_dispatch(x, order).any()
+    nan = torch.full((12, 20), float("nan"), dtype=BF16).cuda()
+    assert not gpu.themis_expert_combine(nan, order, torch.ones(6, 2).cuda()).any()
+    rows, products = gpu.themis_expert_combine_grad(x, nan, order, torch.ones(6, 2).cuda())
+    assert not rows.any() and not products.any()
+    order = gpu.themis_expert_sort(torch.zeros((6, 2), dtype=I32).cuda(), 3)
+    rows, products = gpu.themis_expert_combine_grad(x[:, :0], nan[:, :0], order, torch.ones(6, 2).cuda())
+    assert rows.shape == (12, 0) and not products.any() and gpu.themis_expert_dispatch(x[:, :0], order).shape == (12, 0)
+
+
+def test_weights_of_pairs_without_a_slot_have_no_part(gpu):
+    order, (place, _, _, _) = an_order(gpu, (50, 3), 4, 10, 2)
+    w, y, g = normal((50, 3), F32, 1), normal((40, 30), F32, 2), normal((50, 30), F32, 3)
+    spoiled = torch.where(torch.from_numpy(place) < 0, float("nan"), w)
+    assert torch.isnan(spoiled).any()
+    same(gpu.themis_expert_combine(y.cuda(), order, spoiled.cuda()), gpu.themis_expert_combine(y.cuda(), order, w.cuda()))
+    for a, b in zip(gpu.themis_expert_combine_grad(g.cuda(), y.cuda(), order, spoiled.cuda()),
+                    gpu.themis_expert_combine_grad(g.cuda(), y.cuda(), order, w.cuda())):
+        same(a, b)
+
+
 def test_row_strides(gpu):
     """Tokens in two levels, slots that are every other row, rows at odd addresses, one row for all."""
     order, orders = an_order(gpu, (6, 10, 2), 5, 30, 3)
