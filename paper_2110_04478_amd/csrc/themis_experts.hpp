@@ -847,11 +847,11 @@ combine_grad_kernel(Order o, Rows grad, uint32_t width, Rows y, Rows weights, Ro
   }
   const uint32_t lanes = 1u << shift, lane = threadIdx.x & (lanes - 1u), each = (o.k + kGradPairs - 1) / kGradPairs;
   const uint32_t groups = 256u >> shift, block = blockIdx.x - fills, blocks = gridDim.x - fills;
-  const uint64_t units = (uint64_t)o.n * each;
+  const uint32_t units = o.n * each;   // (no more than pairs)
   for (uint64_t u0 = (uint64_t)block * groups; u0 < units; u0 += (uint64_t)blocks * groups) {
-    const uint64_t unit = u0 + (threadIdx.x >> shift);
+    const uint32_t unit = (uint32_t)u0 + (threadIdx.x >> shift);
     const bool mine = unit < units;
-    const uint32_t t = mine ? (uint32_t)(unit / each) : 0u, j0 = mine ? (uint32_t)(unit % each) * kGradPairs : 0u;
+    const uint32_t t = mine ? unit / each : 0u, j0 = mine ? unit % each * kGradPairs : 0u;
     uint32_t s[kGradPairs];
     float w[kGradPairs], dot[kGradPairs];
 #pragma unroll
@@ -877,13 +877,13 @@ combine_grad_kernel(Order o, Rows grad, uint32_t width, Rows y, Rows weights, Ro
       for (uint32_t u = 0; u < kGradPairs; ++u) {
         if (s[u] >= o.slots) continue;
         if (rows.data) slice.template write_over<kWhole, kAway>(row_at<Y>(rows, s[u]), g * w[u]);
-        float8 x = widen<8>(v[u]), mine = g;
+        float8 a = widen<8>(v[u]), b = g;
         if (!whole) {
-          x = slice.template own<kWhole>(x);
-          mine = slice.template own<kWhole>(mine);
+          a = slice.template own<kWhole>(a);
+          b = slice.template own<kWhole>(b);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dot[u] = __builtin_fmaf(x[i], mine[i], dot[u]);
+        for (int i = 0; i < 8; ++i) dot[u] = __builtin_fmaf(a[i], b[i], dot[u]);
       }
     }
     if (!grad_weights.data) continue;

@@ -66,11 +66,6 @@ int order_status(const themis_expert_order_t* o, Order& view) {
   return THEMIS_OK;
 }
 
-// Rows that are written: n of `width` elements.
-bool target_ok(const themis_rows_t* r, uint64_t n, uint64_t width, bool index = false) {
-  return rows_ok(r, index) && rows_apart(*r, n, width);
-}
-
 // n rows of `width` elements over a grid, `vec` elements a lane.  (Lanes in powers of two for a row: 65 of 128 have
 // work in rows of 520, whose sums of eight take 121 us in place of 97.)
 Spread spread_of(uint64_t n, uint64_t width, uint32_t vec) {

@@ -487,6 +487,22 @@ def test_rows_without_pairs(gpu):
     assert rows.shape == (12, 0) and not products.any() and gpu.themis_expert_dispatch(x[:, :0], order).shape == (12, 0)
 
 
+def test_one_token_without_a_batch(gpu):
+    """Every shape may be a token's alone: [experts], [k], [width]."""
+    logits = normal((40,), F32, 1)
+    weights, chosen = check_gate(gpu, logits, 3, True)
+    grad = gpu.themis_expert_gate_grad(weights, logits.cuda(), chosen)
+    same(grad, gpu.themis_expert_gate_grad(weights[None], logits[None].cuda(), chosen[None])[0])
+    order = check_order(gpu, chosen.cpu(), 40, 2)
+    x = normal((30,), BF16, 2).cuda()
+    rows = gpu.themis_expert_dispatch(x, order)
+    assert all(torch.equal(rows[2 * int(e)], x) for e in chosen) and int(rows.any(1).sum()) == 3
+    back = gpu.themis_expert_combine(rows, order, torch.tensor([0.5, 0.25, 0.25]).cuda())
+    assert torch.equal(back, x)
+    _, products = gpu.themis_expert_combine_grad(x, rows, order, weights)
+    assert products.shape == (3,) and bool((products - x.float().square().sum()).abs().max() <= 32 * U * x.float().square().sum())
+
+
 def test_weights_of_pairs_without_a_slot_have_no_part(gpu):
     order, (place, _, _, _) = an_order(gpu, (50, 3), 4, 10, 2)
     w, y, g = normal((50, 3), F32, 1), normal((40, 30), F32, 2), normal((50, 30), F32, 3)
