@@ -708,8 +708,10 @@ int themis_expert_sort(const themis_rows_t *experts, const themis_expert_order_t
  * Either may be NULL.  (Without weights the gradient of y is
  * themis_expert_dispatch of grad_out.)
  *
- *   order          : as themis_expert_sort filled it; place and source are read, and
- *                    a place or source that is none of the order's is taken as -1
+ *   order          : as themis_expert_sort filled it; place and source are read.  In one
+ *                    that was changed, a place that is no slot is taken as -1, and
+ *                    what is written by slots (out of dispatch, grad_y) takes slot s as
+ *                    pair a's where source[s] is a and place[a] is s, else as no pair's
  *   x, out of combine, grad_out   : n rows of `width`, any of the three types
  *   out of dispatch, y, grad_y    : a row for every slot; grad_y of y's type
  *   weights, grad_weights         : n rows of k, any of the three types

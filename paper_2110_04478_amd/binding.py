@@ -777,7 +777,8 @@ def themis_expert_gate_grad(grad_weights: torch.Tensor, logits: torch.Tensor, ex
 
 @dataclass
 class ExpertOrder:
-    """Pairs (token, its j-th expert) in the order of their experts (themis_expert_sort)."""
+    """Pairs (token, its j-th expert) in the order of their experts (themis_expert_sort).  A pair whose place is
+    set to -1 afterwards has no part in sums, and its slot holds zeros where rows are written by slots."""
     place: torch.Tensor    # i32 [.., k]: slot of a pair, -1 for none
     counts: torch.Tensor   # i32 [n_experts]: pairs of an expert, those without a slot too
     starts: torch.Tensor   # i32 [n_experts + 1]: first slot of an expert; behind the last

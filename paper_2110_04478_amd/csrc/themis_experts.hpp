@@ -751,8 +751,14 @@ expert_sort_kernel(Order o, Rows chosen, uint32_t part, uint32_t parts, const ui
 
 // ---------------------------------------------------------------------------
 // Rows into the order of the experts and back: eight elements a lane.  A place that is no slot (-1, or
-// what a caller wrote there) is none.
+// what a caller wrote there) is none.  What is written by slots goes by both directions: slot s is pair a's
+// where place[a] is s and source[s] is a, and is cleared where that is so for no pair, so that in an order
+// which a caller has changed, too, every slot is written, and once.  (The looks at the other direction: a row
+// of 4,096 bf16 takes as long as without, 100,000 tokens' rows of 64 to six places 23 us for 19.4.)
 // ---------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t source_of(const Order& o, uint32_t s) {
+  return s < o.slots ? (uint32_t)o.source[s] : ~0u;
+}
 
 // sum += x * w, each element rounded once.
 __device__ __forceinline__ void add_product(float8& sum, float8 x, float w) {
@@ -767,7 +773,11 @@ __device__ __forceinline__ void clear_empty_slots(const Order& o, uint32_t block
   const uint32_t lane = threadIdx.x & 63u;
   for (uint64_t s0 = (uint64_t)block * rows; s0 < o.slots; s0 += (uint64_t)blocks * rows) {
     const uint32_t s = (uint32_t)s0 + lane;
-    const bool empty = lane < rows && s < o.slots && (uint32_t)o.source[min(s, o.slots - 1u)] >= o.pairs;
+    bool empty = lane < rows && s < o.slots;
+    if (empty) {
+      const uint32_t pair = (uint32_t)o.source[s];
+      empty = pair >= o.pairs || (uint32_t)o.place[pair] != s;
+    }
     write_zeros<kWhole, kAway, Out>(__ballot(empty), (uint32_t)s0, width, out);
   }
 }
@@ -776,6 +786,7 @@ __device__ __forceinline__ void clear_empty_slots(const Order& o, uint32_t block
 // workgroups clear the slots of no pair.  Bound by memory: 131,072 rows of 4,096 bf16, eight of every row read, in
 // 231 us, 5.2 TB/s, where a fill makes 6.8; slot by slot, in the order of the memory that is written, each row is read
 // eight times from the caches and it takes 300.
+constexpr uint32_t kPlacesAhead = 2;
 template <bool kWhole, bool kAway, typename In, typename Out>
 __global__ void __launch_bounds__(256)
 dispatch_kernel(Order o, Rows x, uint32_t width, Rows out, Spread spread, uint32_t fills, uint32_t fill_rows) {
@@ -785,11 +796,17 @@ dispatch_kernel(Order o, Rows x, uint32_t width, Rows out, Spread spread, uint32
   }
   spread_rows(spread, blockIdx.x - fills, o.n, [&](uint32_t t, uint32_t lane) {
     const Slice<kVecOf<In, Out>> slice(0, lane, spread.lanes, width);
-    const int32_t* place = o.place + (uint64_t)t * o.k;
+    const uint32_t first = t * o.k;
     const float8 v = widen<8>(slice.template read<kWhole>(row_at<const In>(x, t)));
-    for (uint32_t j = 0; j < o.k; ++j) {
-      const uint32_t s = (uint32_t)place[j];
-      if (s < o.slots) slice.template write_over<kWhole, kAway>(row_at<Out>(out, s), v);
+    for (uint32_t j0 = 0; j0 < o.k; j0 += kPlacesAhead) {
+      uint32_t s[kPlacesAhead], source[kPlacesAhead];
+#pragma unroll
+      for (uint32_t u = 0; u < kPlacesAhead; ++u) s[u] = j0 + u < o.k ? (uint32_t)o.place[first + j0 + u] : ~0u;
+#pragma unroll
+      for (uint32_t u = 0; u < kPlacesAhead; ++u) source[u] = source_of(o, s[u]);
+#pragma unroll
+      for (uint32_t u = 0; u < kPlacesAhead; ++u)
+        if (source[u] == first + j0 + u) slice.template write_over<kWhole, kAway>(row_at<Out>(out, s[u]), v);
     }
   });
 }
@@ -852,7 +869,7 @@ combine_grad_kernel(Order o, Rows grad, uint32_t width, Rows y, Rows weights, Ro
     const uint32_t unit = (uint32_t)u0 + (threadIdx.x >> shift);
     const bool mine = unit < units;
     const uint32_t t = mine ? unit / each : 0u, j0 = mine ? unit % each * kGradPairs : 0u;
-    uint32_t s[kGradPairs];
+    uint32_t s[kGradPairs], source[kGradPairs];
     float w[kGradPairs], dot[kGradPairs];
 #pragma unroll
     for (uint32_t u = 0; u < kGradPairs; ++u) {
@@ -861,6 +878,8 @@ combine_grad_kernel(Order o, Rows grad, uint32_t width, Rows y, Rows weights, Ro
       w[u] = float_at(weights, t, j);
       dot[u] = 0.0f;
     }
+#pragma unroll
+    for (uint32_t u = 0; u < kGradPairs; ++u) source[u] = rows.data ? source_of(o, s[u]) : ~0u;
     for (uint32_t c = 0; c < width; c += lanes * kLaneElements) {
       const Slice<kVecOf<G, Y>> slice(c, lane, lanes, width);
       if (!slice.any()) continue;
@@ -876,7 +895,7 @@ combine_grad_kernel(Order o, Rows grad, uint32_t width, Rows y, Rows weights, Ro
 #pragma unroll
       for (uint32_t u = 0; u < kGradPairs; ++u) {
         if (s[u] >= o.slots) continue;
-        if (rows.data) slice.template write_over<kWhole, kAway>(row_at<Y>(rows, s[u]), g * w[u]);
+        if (source[u] == t * o.k + j0 + u) slice.template write_over<kWhole, kAway>(row_at<Y>(rows, s[u]), g * w[u]);
         float8 a = widen<8>(v[u]), b = g;
         if (!whole) {
           a = slice.template own<kWhole>(a);

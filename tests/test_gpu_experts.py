@@ -552,6 +552,44 @@ def test_an_order_that_is_none_is_not_followed(gpu):
     assert products[3, 0] == 0 and products[4, 1] == 0
 
 
+CHANGES = dict(place_none=lambda place, source: place.view(-1)[3:9:2].fill_(-1),
+               place_outside=lambda place, source: place.view(-1)[3:9:2].fill_(10 ** 6),
+               place_of_another=lambda place, source: place.view(-1)[3:6].copy_(place.view(-1)[6:9].clone()),
+               source_none=lambda place, source: source[:5].fill_(-1),
+               source_outside=lambda place, source: source[2:7].fill_(10 ** 6),
+               source_of_another=lambda place, source: source[2:4].copy_(source[4:6].clone()),
+               places_swapped=lambda place, source: place.copy_(place.flip(0).clone()),
+               all_sources_none=lambda place, source: source.fill_(-1))
+
+
+@pytest.mark.parametrize("width", [5, 24, 520, 2049])
+@pytest.mark.parametrize("capacity", [0, 14])
+@pytest.mark.parametrize("change", list(CHANGES))
+def test_rows_by_slots_of_an_order_that_was_changed(gpu, change, capacity, width):
+    """Slot s is pair a's where source[s] is a and place[a] is s, and holds zeros otherwise: every slot is
+    written, and by one pair."""
+    order, orders = an_order(gpu, (40, 3), 9, capacity, 1)
+    CHANGES[change](order.place, order.source)
+    place, source = order.place.cpu().view(-1).long(), order.source.cpu().long()
+    slots, pairs = len(source), place.numel()
+    inside = (source >= 0) & (source < pairs)
+    own = inside & (place[torch.where(inside, source, 0)] == torch.arange(slots))
+    assert int(own.sum()) < int((orders[3] >= 0).sum())
+    agreed = torch.where(own, source, -1).numpy()
+    for kind in (F32, BF16):
+        x, w, y = normal((40, width), kind, 1), normal((40, 3), F32, 2), normal((slots, width), kind, 3)
+        out = torch.full((slots, width), float("nan"), dtype=kind).cuda()
+        same(gpu.themis_expert_dispatch(x.cuda(), order, out=out), dispatch_of(x, place.view(40, 3).numpy(), agreed, kind))
+        want = (x.float()[torch.from_numpy(agreed).clamp(min=0) // 3] *
+                w.reshape(-1)[torch.from_numpy(agreed).clamp(min=0)][:, None])
+        want[~own] = 0
+        dx, dy, dw = x.cuda(), y.cuda(), w.cuda()
+        for need in (True, False):
+            spoiled = torch.full_like(dy, float("nan"))
+            del spoiled   # (the result's memory: what is not written shows)
+            same(gpu.themis_expert_combine_grad(dx, dy, order, dw, need_weights=need)[0], want.to(kind))
+
+
 @pytest.mark.parametrize("kind,width,k,capacity", [(BF16, 4096, 3, 0), (F32, 1030, 2, 9000), (F16, 500, 8, 0)])
 def test_rows_beyond_the_last_cache_level(gpu, kind, width, k, capacity):
     """Read another way there: the same as in two calls on half of the columns, which are not; products
