@@ -777,7 +777,8 @@ def themis_expert_gate_grad(grad_weights: torch.Tensor, logits: torch.Tensor, ex
 
 @dataclass
 class ExpertOrder:
-    """Pairs (token, its j-th expert) in the order of their experts (themis_expert_sort).  A pair whose place is
+    """Pairs (token, its j-th expert) in the order of their experts (themis_expert_sort), pieces of one
+    allocation; counts and starts may be changed once they are there, nothing here reads them.  A pair whose place is
     set to -1 afterwards has no part in sums, and its slot holds zeros where rows are written by slots."""
     place: torch.Tensor    # i32 [.., k]: slot of a pair, -1 for none
     counts: torch.Tensor   # i32 [n_experts]: pairs of an expert, those without a slot too
@@ -827,7 +828,8 @@ def themis_expert_sort(experts: torch.Tensor, n_experts: int, capacity: int = 0,
     first = room.data_ptr()
     at, size = (first, 4 * own) if workspace is None else (workspace.data_ptr(),
                                                            workspace.numel() * workspace.element_size())
-    _, place, counts, starts, source = torch.split_with_sizes(room, (own, pairs, n_experts, n_experts + 1, slots))
+    # (pieces with version numbers of their own: a caller may change the counts before a backward reads the places)
+    _, place, counts, starts, source = torch.unsafe_split_with_sizes(room, (own, pairs, n_experts, n_experts + 1, slots))
     first += 4 * own
     order = _ExpertOrder(n, k, n_experts, capacity, first, first + 4 * pairs, first + 4 * (pairs + n_experts),
                          first + 4 * (pairs + 2 * n_experts + 1))

@@ -118,6 +118,23 @@ def test_what_changed_before_the_backward_is_an_error(layers):
         out.sum().backward()
 
 
+@pytest.mark.parametrize("capacity", [0, 6])
+def test_counts_may_change_before_the_backward(layers, capacity):
+    """Summed over ranks in place, say: the gradients do not read them."""
+    x, w = normal((30, 16), 1).requires_grad_(), normal((30, 2), 2).requires_grad_()
+    chosen = torch.arange(60, dtype=torch.int32, device="cuda").view(30, 2) % 5
+    grads = []
+    for change in (False, True):
+        order = layers.sort(chosen, 5, capacity)
+        out = layers.combine(layers.dispatch(x, order), order, w)
+        if change:
+            order.counts.mul_(8)
+            order.starts.add_(3)
+            assert order.counts.tolist() == [96] * 5 and order.place.max() < 60
+        grads.append(torch.autograd.grad(out.square().sum(), (x, w)))
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
+
+
 def test_dropout_of_zero_gradients_and_of_add_alone(layers):
     x, held = normal((9, 33), 1), normal((9, 33), 2).requires_grad_()
     layers.dropout(x, 0.5, 1, 2, add=held).sum().backward()
