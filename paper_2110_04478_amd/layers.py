@@ -82,7 +82,8 @@ def dispatch(x: torch.Tensor, order: binding.ExpertOrder) -> torch.Tensor:
 class _Combine(torch.autograd.Function):
     @staticmethod
     def forward(ctx, y, weights, order, dtype):
-        ctx.save_for_backward(y, weights, order.place, order.source)
+        # (only the weights' gradient reads y)
+        ctx.save_for_backward(y if ctx.needs_input_grad[1] else None, weights, order.place, order.source)
         ctx.args = order, y.dtype
         return binding.themis_expert_combine(y, order, weights, out_dtype=dtype)
 
@@ -93,6 +94,8 @@ class _Combine(torch.autograd.Function):
         order, dtype = ctx.args
         if weights is None:
             return binding.themis_expert_dispatch(grad, order, out_dtype=dtype), None, None, None
+        if y is None:   # (of its type and size)
+            y = grad.new_empty((1, grad.shape[-1]), dtype=dtype).expand(order.slots, -1)
         rows, products = binding.themis_expert_combine_grad(grad, y, order, weights, ctx.needs_input_grad[0],
                                                             ctx.needs_input_grad[1])
         return rows, products, None, None

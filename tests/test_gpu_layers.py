@@ -135,6 +135,29 @@ def test_counts_may_change_before_the_backward(layers, capacity):
     assert all(torch.equal(a, b) for a, b in zip(*grads))
 
 
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("weighted", [False, True])
+@pytest.mark.parametrize("width", [1, 24])
+def test_rows_that_no_gradient_reads_are_not_kept(layers, width, weighted, kind):
+    """Without gradients of weights y may change, and its memory is free, before the backward."""
+    leaf, w = normal((60, width), 1, dtype=kind).requires_grad_(), normal((30, 2), 2) if weighted else None
+    order = layers.sort(torch.arange(60, dtype=torch.int32, device="cuda").view(30, 2) % 5, 5)
+    g = normal((30, width), 3)
+    grads = []
+    for change in (False, True):
+        y = leaf * 1
+        out = layers.combine(y, order, w, F32)
+        if change:
+            y.mul_(2)
+        grads.append(torch.autograd.grad(out, leaf, g)[0])
+    assert grads[0].dtype == kind and grads[0].shape == (60, width) and torch.equal(*grads)
+    y = leaf * 1
+    out = layers.combine(y, order, normal((30, 2), 2).requires_grad_())
+    y.mul_(2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(out, leaf, g.to(kind))
+
+
 def test_dropout_of_zero_gradients_and_of_add_alone(layers):
     x, held = normal((9, 33), 1), normal((9, 33), 2).requires_grad_()
     layers.dropout(x, 0.5, 1, 2, add=held).sum().backward()
