@@ -154,9 +154,9 @@ def lib():
 
 
 class ThemisError(RuntimeError):
-    def __init__(self, status: int):
+    def __init__(self, status: int, why: str = ""):
         self.status = status
-        super().__init__(f"themis: {lib().themis_status_string(status).decode()} ({status})")
+        super().__init__(f"themis: {lib().themis_status_string(status).decode()} ({status}){why and ': ' + why}")
 
 
 def _check(status: int):

@@ -33,7 +33,9 @@ def _apply(function, leaves, *args):
             if t is not None and t.requires_grad and t.is_leaf:
                 nodes.append(torch.autograd.graph.get_gradient_edge(t).node)
                 captured = torch.cuda.is_current_stream_capturing()
-                binding._need(nodes[-1].metadata.setdefault("captured", captured) or not captured)
+                if not nodes[-1].metadata.setdefault("captured", captured) and captured:
+                    raise binding.ThemisError(binding.INVALID_ARGUMENT,
+                                              "captured while an eager graph of the same leaf lives")
     return function.apply(*args)
 
 

@@ -157,6 +157,29 @@ def test_tensors_on_the_host_are_refused(binding):
             call()
 
 
+def test_a_capture_beside_an_eager_graph_says_so(binding, monkeypatch):
+    """Not as a wrong shape does: what has to change is the program's order, not the call."""
+    from paper_2110_04478_amd import layers
+
+    class Same(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            return x.clone()
+
+        @staticmethod
+        def backward(ctx, grad):
+            return grad
+
+    x = torch.ones(3, requires_grad=True)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    alive = layers._apply(Same, (x,), x)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(binding.ThemisError, match="invalid argument.*eager graph of the same leaf") as e:
+        layers._apply(Same, (x,), x)
+    assert e.value.status == binding.INVALID_ARGUMENT and alive.requires_grad
+    assert str(binding.ThemisError(-1)) == "themis: invalid argument (-1)"
+
+
 CALLER = r"""
 import ctypes, json, sys
 ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
