@@ -44,8 +44,9 @@ def feed_forward(p, x):
     if "router" not in p:
         return torch.relu(x @ p["up"].t()) @ p["down"].t()
     n_experts, width = p["up"].shape[:2]
-    capacity = math.ceil(CAPACITY * CHOSEN * x[..., 0].numel() / n_experts)
-    weights, chosen = layers.gate(x @ p["router"].t(), CHOSEN)
+    k = min(CHOSEN, n_experts)
+    capacity = math.ceil(CAPACITY * k * x[..., 0].numel() / n_experts)
+    weights, chosen = layers.gate(x @ p["router"].t(), k)
     order = layers.sort(chosen, n_experts, capacity)
     rows = layers.dispatch(x, order).view(n_experts, capacity, width)
     rows = torch.bmm(torch.relu(torch.bmm(rows, p["up"])), p["down"])

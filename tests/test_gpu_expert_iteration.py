@@ -55,3 +55,20 @@ def test_its_gradients(example):
     want = (rows + torch.where(kept, want / 0.75, 0.0)).view(x.shape)
     for a, b in zip(got, torch.autograd.grad(want, [z] + [q[k] for k in names], g.cpu().double())):
         assert float((a.cpu().double() - b).abs().max()) <= 2560 * 2.0 ** -24 * float(b.abs().max())
+
+
+@pytest.mark.parametrize("experts", [1, 2, 3])
+def test_few_experts(example, experts):
+    """Fewer than a token's choices, too; of one expert the layer is that expert's, every weight 1."""
+    got = example.main(steps=2, vocab=100, width=32, batch=4, length=24, experts=experts, dropout=0.1)
+    assert all(0 < x < float("inf") for x in got["losses"] + got["norms"])
+    if experts == 1:
+        p = example.model(50, 32, "cuda", 3, 1)
+        x = torch.randn((2, 20, 32), generator=torch.Generator().manual_seed(5)).cuda()
+        y = example.feed_forward(p, x).detach().cpu().double()
+        z, up, down = x.cpu().double(), p["up"][0].detach().cpu().double(), p["down"][0].detach().cpu().double()
+        want = torch.relu(z @ up) @ down
+        # sums of 32 and 128 terms in binary32 (and the sign of a hidden value below its error), relative to
+        # the terms' magnitudes
+        size = (z.abs() @ up.abs()) @ down.abs()
+        assert bool(((y - want).abs() <= (32 + 128 + 8) * 2.0 ** -24 * size).all())
