@@ -31,8 +31,9 @@ SEED = 11
 def model(vocab, width, device, seed, experts=0):
     g = torch.Generator().manual_seed(seed)
 
-    def weight(*shape):
-        return torch.nn.Parameter((torch.randn(shape, generator=g) / math.sqrt(shape[-1])).to(device))
+    def weight(*shape):   # (by what a sum goes over: a row, or of an expert's matrix, which stands to the right, a column)
+        terms = shape[-1] if len(shape) == 2 else shape[-2]
+        return torch.nn.Parameter((torch.randn(shape, generator=g) / math.sqrt(terms)).to(device))
 
     if experts:
         return dict(table=weight(vocab, width), router=weight(experts, width), up=weight(experts, width, 4 * width),
