@@ -238,3 +238,20 @@ def test_every_accepted_size_is_launched(binding, tmp_path):
         pairs, slots = call[1] * call[2], call[3] * call[4] if call[4] else call[1] * call[2]
         assert (status == 0) == (pairs <= MOST and slots <= MOST or call[0] in ("gate", "dropout")), (call, status)
         assert bool(found) == (status == 0), (call, status, found)
+
+
+def test_lists_that_one_workgroup_sorts(binding, tmp_path):
+    """Up to 8,192 pairs one launch without a workspace, beyond them two."""
+    (tmp_path / "r.c").write_text(RECORDER)
+    (tmp_path / "call.py").write_text(CALLER)
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-o", str(tmp_path / "r.so"), str(tmp_path / "r.c"), "-ldl"], check=True)
+    calls = [("sort", n, k, e, c, 0) for n, k in ((8191, 1), (8192, 1), (4096, 2), (8193, 1), (2731, 3)) for e in (1, 61, 1024)
+             for c in (0, 7)]
+    out = subprocess.run([sys.executable, str(tmp_path / "call.py"), str(tmp_path / "r.so"), json.dumps(calls)],
+                         env=dict(os.environ, PYTHONPATH=ROOT), check=True, capture_output=True, text=True).stdout
+    got = [part.splitlines() for part in out.split("call\n")[1:]]
+    assert len(got) == len(calls)
+    size = binding.lib().themis_expert_sort_workspace_bytes
+    for (_, n, k, e, _, _), lines in zip(calls, got):
+        assert lines[-1] == "status 0" and len(lines) == (2 if n * k <= 8192 else 3), (n, k, e, lines)
+        assert (size(n, k, e) > 0) == (n * k > 8192)

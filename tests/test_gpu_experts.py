@@ -223,6 +223,22 @@ def test_gate_gradient_types(gpu, kind, out):
         check_gate_grad(gpu, normal((77, 5), grad, 2), x, gate_64(x, 5, True)[1].to(index), False, out)
 
 
+@pytest.mark.parametrize("experts", [65, 130, 300, 1001])
+@pytest.mark.parametrize("out", [F32, BF16, F16])
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+def test_gate_gradient_types_of_several_chunks(gpu, kind, out, experts):
+    """Two and four accesses a lane, the last one moved back; masked logits, in it too; a row with none left."""
+    x = normal((50, experts), kind, experts, 3.0)
+    g = torch.Generator().manual_seed(experts)
+    x[torch.rand(x.shape, generator=g) < torch.linspace(0, 1, 50)[:, None]] = -INF
+    x[3, -8:], x[4, -5:], x[5, :-3], x[6] = -INF, -INF, -INF, -INF
+    for k in (3, 8, 20):
+        chosen = gate_64(x, k, True)[1]
+        assert bool((chosen[6] == -1).all())
+        for renormalize in (True, False):
+            check_gate_grad(gpu, normal((50, k), F32, 2), x, chosen.to(I32), renormalize, out)
+
+
 @pytest.mark.parametrize("renormalize", [True, False])
 def test_gate_gradient_lists(gpu, renormalize):
     """Experts that stand twice, none, numbers outside; more chosen than lanes; masked logits."""
@@ -308,6 +324,18 @@ def choices(shape, n_experts, seed, dtype=I32, outside=0.0, hot=0.0):
 @pytest.mark.parametrize("n,k", [(1, 1), (1, 8), (7, 3), (64, 1), (1000, 2), (5000, 8), (40960, 1), (40961, 1), (70001, 3)])
 def test_order_sizes(gpu, n, k, n_experts, capacity):
     check_order(gpu, choices((n, k), n_experts, n + k, outside=0.1), n_experts, capacity)
+
+
+@pytest.mark.parametrize("index", [I32, I64])
+@pytest.mark.parametrize("n_experts", [1, 8, 61, 1024])
+@pytest.mark.parametrize("pairs", [1023, 1024, 1025, 4095, 4096, 4097, 6000, 8191, 8192, 8193, 12289])
+def test_order_around_one_workgroup(gpu, pairs, n_experts, index):
+    """Turns of a wavefront, one and several, in one workgroup, and the first lists that two launches sort."""
+    for capacity in (0, 37, 3000):
+        for outside, hot in ((0.0, 0.0), (0.2, 0.0), (0.0, 0.7), (0.1, 1.0)):
+            check_order(gpu, choices((pairs, 1), n_experts, pairs, index, outside, hot), n_experts, capacity)
+    if pairs % 3 == 0:
+        check_order(gpu, choices((pairs // 3, 3), n_experts, pairs, index, 0.1, 0.3), n_experts, 11)
 
 
 @pytest.mark.parametrize("index", [I32, I64])
@@ -630,6 +658,30 @@ def test_places_beyond_32_bits(gpu):
         assert torch.equal(back[s:s + (1 << 17)], rows[s:s + (1 << 17)] * 0.125)
     norms = x.double().square().sum(1, keepdim=True)
     assert bool(((products.double() - norms).abs() <= (width + 3) * U * norms).all())
+
+
+def test_rows_in_several_segments_of_a_grid(gpu):
+    """More lanes than 2^31: long rows, then many short ones, there and back."""
+    n, width = 515, 1 << 25
+    base = torch.randn(width + n, generator=torch.Generator(device="cuda").manual_seed(4), device="cuda").to(BF16)
+    x = base.as_strided((n, width), (1, 1))   # (row t is base from t on)
+    order = gpu.themis_expert_sort(torch.arange(n - 1, -1, -1, device="cuda", dtype=I32)[:, None], n)
+    rows = gpu.themis_expert_dispatch(x, order)
+    for t in range(n):
+        assert torch.equal(rows[n - 1 - t], base[t:t + width]), t
+    sums = gpu.themis_expert_combine(rows, order, torch.full((n, 1), 0.5, device="cuda"))
+    half = base * 0.5
+    for t in range(n):
+        assert torch.equal(sums[t], half[t:t + width]), t
+    del rows, sums
+    n, width = (2 ** 31 - 257) // 2 + 3000, 9
+    base = torch.randn(n + 8, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda", dtype=F32).to(BF16)
+    x = base.as_strided((n, width), (1, 1))
+    order = gpu.themis_expert_sort(torch.zeros((1, 1), device="cuda", dtype=I32).expand(n, 1), 1)
+    for got in (gpu.themis_expert_dispatch(x, order), gpu.themis_expert_combine(x, order)):
+        for t in range(0, n, 1 << 26):
+            assert torch.equal(got[t:t + (1 << 26)], x[t:t + (1 << 26)]), t
+        del got
 
 
 def test_equal_calls_give_equal_bits(gpu):
