@@ -782,12 +782,12 @@ __device__ __forceinline__ void clear_empty_slots(const Order& o, uint32_t block
   }
 }
 
-// themis_expert_dispatch: a row is read once and written to its token's slots; the first `fills`
-// workgroups clear the slots of no pair.  Bound by memory: 131,072 rows of 4,096 bf16, eight of every row read, in
-// 231 us, 5.2 TB/s, where a fill makes 6.8; slot by slot, in the order of the memory that is written, each row is read
-// eight times from the caches and it takes 300.
-constexpr uint32_t kPlacesAhead = 2;
-template <bool kWhole, bool kAway, typename In, typename Out>
+// themis_expert_dispatch: a row is read once and written to its token's slots, kAhead places looked up in front of
+// the writes; the first `fills` workgroups clear the slots of no pair.  Bound by memory: 131,072 rows of 4,096 bf16,
+// eight of every row read, in 230 us, 5.3 TB/s, where a fill makes 6.8; slot by slot, in the order of the memory that
+// is written, each row is read eight times from the caches and it takes 300.
+constexpr int kOneWrite = 0x0F71;   // s_waitcnt: at most one access to memory is under way
+template <bool kWhole, bool kAway, int kAhead, typename In, typename Out>
 __global__ void __launch_bounds__(256)
 dispatch_kernel(Order o, Rows x, uint32_t width, Rows out, Spread spread, uint32_t fills, uint32_t fill_rows) {
   if (blockIdx.x < fills) {
@@ -798,15 +798,20 @@ dispatch_kernel(Order o, Rows x, uint32_t width, Rows out, Spread spread, uint32
     const Slice<kVecOf<In, Out>> slice(0, lane, spread.lanes, width);
     const uint32_t first = t * o.k;
     const float8 v = widen<8>(slice.template read<kWhole>(row_at<const In>(x, t)));
-    for (uint32_t j0 = 0; j0 < o.k; j0 += kPlacesAhead) {
-      uint32_t s[kPlacesAhead], source[kPlacesAhead];
+    for (uint32_t j0 = 0; j0 < o.k; j0 += kAhead) {
+      uint32_t s[kAhead], source[kAhead];
 #pragma unroll
-      for (uint32_t u = 0; u < kPlacesAhead; ++u) s[u] = j0 + u < o.k ? (uint32_t)o.place[first + j0 + u] : ~0u;
+      for (uint32_t u = 0; u < kAhead; ++u) s[u] = j0 + u < o.k ? (uint32_t)o.place[first + j0 + u] : ~0u;
 #pragma unroll
-      for (uint32_t u = 0; u < kPlacesAhead; ++u) source[u] = source_of(o, s[u]);
+      for (uint32_t u = 0; u < kAhead; ++u) source[u] = source_of(o, s[u]);
 #pragma unroll
-      for (uint32_t u = 0; u < kPlacesAhead; ++u)
-        if (source[u] == first + j0 + u) slice.template write_over<kWhole, kAway>(row_at<Out>(out, s[u]), v);
+      for (uint32_t u = 0; u < kAhead; ++u)
+        if (source[u] == first + j0 + u) {
+          slice.template write_over<kWhole, kAway>(row_at<Out>(out, s[u]), v);
+          // (the memory takes the writes of many rows the better the fewer of them a wavefront has under way:
+          // eight at once 244 us; two places, then two writes 238)
+          if (kAhead > 2) __builtin_amdgcn_s_waitcnt(kOneWrite);
+        }
     }
   });
 }
