@@ -682,7 +682,8 @@ typedef struct themis_expert_order {
 /*
  * themis_expert_sort -- fills in place, counts, starts and source.
  *
- *   experts   : n rows of k numbers, THEMIS_I32 / _I64
+ *   experts   : n rows of k numbers, THEMIS_I32 / _I64; what is written overlaps nothing
+ *               else
  *   workspace : themis_expert_sort_workspace_bytes(n, k, n_experts) bytes, 16-byte
  *               aligned, untouched until the stream has drained, one per call in
  *               flight.

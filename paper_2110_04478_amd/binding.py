@@ -816,6 +816,7 @@ def themis_expert_sort(experts: torch.Tensor, n_experts: int, capacity: int = 0,
     device = experts.get_device()
     _need(device >= 0 and experts.dim() >= 1 and experts.dtype in _INDEXES and n_experts >= 1 and capacity >= 0 and
           (workspace is None or (workspace.get_device() == device and workspace.is_contiguous())))
+    _need_apart(workspace, experts)
     stream = _stream_here(device)
     k, pairs = experts.shape[-1], experts.numel()
     n = pairs // k if k else experts.shape[:-1].numel()

@@ -203,6 +203,21 @@ def test_refusals(layers):
             pytest.fail("call %d was taken" % n)
 
 
+def test_a_workspace_on_the_list_is_refused(layers):
+    """The counts of the parts would be written over experts that are read again after them."""
+    from paper_2110_04478_amd import binding
+    n = 20000
+    need = binding.themis_expert_sort_workspace_bytes(n, 1, 16)
+    room = torch.zeros(need // 4 + n, dtype=torch.int32, device="cuda")
+    chosen = room[need // 4:].random_(0, 16).view(n, 1)
+    want = binding.themis_expert_sort(chosen.clone(), 16)
+    for bad in (room, room[need // 4:], room[4:need // 4 + 4]):
+        with pytest.raises(binding.ThemisError):
+            binding.themis_expert_sort(chosen, 16, workspace=bad)
+    beside = binding.themis_expert_sort(chosen, 16, workspace=room[:need // 4])
+    assert torch.equal(beside.place, want.place) and torch.equal(beside.source, want.source)
+
+
 def test_on_other_streams(layers):
     """An order made on one stream and used on another, and given up at once: its memory waits."""
     from paper_2110_04478_amd import binding
