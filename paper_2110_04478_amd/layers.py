@@ -8,10 +8,10 @@ experts and back, elements dropped by a counter.
 
 Differentiable once: a derivative through a gradient raises an error.
 
-A backward can be captured into a graph with its forward while no eager graph of the same leaves lives
-(torch's engine brings the eager graph's stream into the capture and ends the process).  Where such a leaf
-is an argument of these functions both times the captured call is refused; of leaves that only other
-functions read they know nothing."""
+A backward can be captured into a graph with its forward while no eager graph of the same leaves lives,
+and none that was captured on another stream (torch's engine brings that graph's stream into the capture
+and ends the process).  Where such a leaf is an argument of these functions both times the captured call
+is refused; of leaves that only other functions read they know nothing."""
 from __future__ import annotations
 
 from typing import Optional
@@ -26,16 +26,20 @@ sort = binding.themis_expert_sort
 
 def _apply(function, leaves, *args):
     """function.apply(*args); what accumulates the gradients of the leaves among `leaves` is marked
-    with whether it was made in a capture."""
+    with the stream of the capture that it was made in, if it was."""
     nodes = []   # (held until the graph holds them)
     if torch.is_grad_enabled():
         for t in leaves:
             if t is not None and t.requires_grad and t.is_leaf:
                 nodes.append(torch.autograd.graph.get_gradient_edge(t).node)
-                captured = torch.cuda.is_current_stream_capturing()
-                if not nodes[-1].metadata.setdefault("captured", captured) and captured:
+                here = None
+                if torch.cuda.is_current_stream_capturing():
+                    here = torch._C._cuda_getCurrentRawStream(t.get_device()) if t.is_cuda else -1
+                made = nodes[-1].metadata.setdefault("captured", here)
+                if here is not None and made != here:
                     raise binding.ThemisError(binding.INVALID_ARGUMENT,
-                                              "captured while an eager graph of the same leaf lives")
+                                              "captured while %s graph of the same leaf lives" %
+                                              ("an eager" if made is None else "another stream's"))
     return function.apply(*args)
 
 

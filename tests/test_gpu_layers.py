@@ -328,3 +328,22 @@ def test_a_capture_beside_an_eager_graph_of_a_leaf_is_refused(layers, monkeypatc
             call()
             with torch.no_grad():
                 call()
+
+
+def test_captures_on_two_streams_beside_each_other_are_refused(layers, monkeypatch):
+    """While what the first one captured of a leaf lives.  (The captures are only said to run, as above.)"""
+    from paper_2110_04478_amd import binding
+    x = normal((8, 16), 1).requires_grad_()
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    one, other = torch.cuda.Stream(), torch.cuda.Stream()
+    assert one.cuda_stream != other.cuda_stream
+    with torch.cuda.stream(one):
+        alive = layers.dropout(x, 0.5, 1, 2)
+        layers.dropout(x, 0.5, 1, 3)   # (the same stream: as ever)
+    with torch.cuda.stream(other):
+        with pytest.raises(binding.ThemisError, match="another stream's graph of the same leaf"):
+            layers.dropout(x, 0.5, 1, 2)
+        del alive
+        layers.dropout(x, 0.5, 1, 2)
+    torch.cuda.synchronize()
