@@ -74,8 +74,8 @@ __device__ __forceinline__ void put_number(const Rows& rows, uint32_t r, uint32_
 // 2^shift lanes take a token, each kOwn adjacent logits in registers; k times the largest is found
 // (over a lane's own, then over the lanes) and taken out.  Logits are compared as whole numbers
 // that are ordered as the values are; those of 16 bits carry their index in the lower half, smaller ones
-// first, so that one maximum gives both.  Bound by its instructions, for more than eight experts, as few models
-// have: 65,536 tokens on 256 experts, 16 of them (bf16), 45 us, 64 of them 128.
+// first, so that one maximum gives both.  For more than eight experts.  Bound by its instructions, which leave no
+// cycle free: 65,536 tokens on 256 experts, 16 of them (bf16), 45 us, 64 of them 129.
 // ---------------------------------------------------------------------------
 constexpr uint32_t kMostExperts = 1024;
 constexpr uint32_t kMostChosen = 64;
@@ -194,8 +194,8 @@ gate_kernel(Rows logits, uint32_t experts, uint32_t n, uint32_t k, bool renormal
 // An entry is a number that is ordered as (logit, index from the end) is: of logits of 16 bits
 // a whole number, the logit as a signed one (so that -0 is 0) over its index, of binary32 a binary64
 // number, the logit with its index in the last of the 29 bits that it leaves free.
-// 65,536 tokens on 256 experts, eight of them (bf16): 12.8 us, of which the logits' bytes need 8; by k
-// rounds of a maximum 33.
+// 65,536 tokens on 256 experts, eight of them (bf16): 11.7 us, of which the logits' bytes need 8, by k
+// rounds of a maximum 33; over all 18.  Bound by instructions (on 86 % of the cycles, over all 97 %).
 // ---------------------------------------------------------------------------
 constexpr uint32_t kMostListed = 8;
 
@@ -443,8 +443,10 @@ gate_list_kernel(Rows logits, uint32_t experts, uint32_t n, uint32_t k, Rows wei
 //   over all:         dl[e] = sum over j with e_j == e of w_j dw_j  -  p_e sum_i w_i dw_i
 // The lanes of a token hold its logits in the gate's chunks (over the chosen none: those of the list are read
 // by themselves), and a pair (expert, gradient) each, whose term goes to the expert's lane through LDS.
-// 65,536 tokens on 256 experts, eight of them (bf16): 15.6 us over the chosen (their bytes need 8), 27 over all
-// (15; bound by the exponentials); with every pair compared with every register 37 and 42.
+// 65,536 tokens on 256 experts, eight of them (bf16): 15.9 us over the chosen (their bytes need 8), 27 over all
+// (15); with every pair compared with every register 37 and 42.  Bound by waits: over the chosen the terms' 32 KB of
+// LDS leave room for five workgroups, which issue on 32 % of the cycles, over all 176 registers for two wavefronts a
+// SIMD, which issue on 60 %; a third of the instructions are the exponentials'.
 // ---------------------------------------------------------------------------
 template <typename T, typename Out, int kChunks, bool kAll>
 __global__ void __launch_bounds__(256)
@@ -563,9 +565,9 @@ gate_grad_kernel(Rows grad, Rows logits, uint32_t experts, Rows chosen, uint32_t
 //
 // As the table gradient's sort, in one pass: the workgroups count the experts of their parts of the
 // list, then every workgroup finds from all counts where its part's pairs go.  One workgroup does both
-// where the list is short.  Bound by waits: of 1,048,576 pairs on 256 experts the count takes 3 us, the rest 15.7: 4 to
-// the first barrier, 4.5 for the counts of 256 parts, 4 for the ranks, 3 for numbers of pairs that are written in
-// runs of 16.
+// where the list is short.  Bound by waits: of 1,048,576 pairs on 256 experts the count takes 3 us, the rest 15.7 (each by
+// itself; the call 17.2): 4 to the first barrier, 4.5 for the counts of 256 parts, 4 for the ranks, 3 for numbers of
+// pairs that are written in runs of 16.
 // ---------------------------------------------------------------------------
 struct Order {
   uint32_t n, k, pairs, experts, capacity, slots;   // capacity 0: packed
@@ -753,8 +755,8 @@ expert_sort_kernel(Order o, Rows chosen, uint32_t part, uint32_t parts, const ui
 // Rows into the order of the experts and back: eight elements a lane.  A place that is no slot (-1, or
 // what a caller wrote there) is none.  What is written by slots goes by both directions: slot s is pair a's
 // where place[a] is s and source[s] is a, and is cleared where that is so for no pair, so that in an order
-// which a caller has changed, too, every slot is written, and once.  (The looks at the other direction: a row
-// of 4,096 bf16 takes as long as without, 100,000 tokens' rows of 64 to six places 23 us for 19.4.)
+// which a caller has changed, too, every slot is written, and once.  (The looks at the other direction: rows of
+// 4,096 bf16 take as long as without, 100,000 tokens' rows of 64 to six places 23 us for 19.4.)
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t source_of(const Order& o, uint32_t s) {
   return s < o.slots ? (uint32_t)o.source[s] : ~0u;
@@ -784,7 +786,7 @@ __device__ __forceinline__ void clear_empty_slots(const Order& o, uint32_t block
 
 // themis_expert_dispatch: a row is read once and written to its token's slots, kAhead places looked up in front of
 // the writes; the first `fills` workgroups clear the slots of no pair.  Bound by memory: 131,072 rows of 4,096 bf16,
-// eight of every row read, in 230 us, 5.3 TB/s, where a fill makes 6.8; slot by slot, in the order of the memory that
+// eight of every row read, in 228 us, 5.3 TB/s, where a fill makes 6.8; slot by slot, in the order of the memory that
 // is written, each row is read eight times from the caches and it takes 300.
 constexpr int kOneWrite = 0x0F71;   // s_waitcnt: at most one access to memory is under way
 template <bool kWhole, bool kAway, int kAhead, typename In, typename Out>
